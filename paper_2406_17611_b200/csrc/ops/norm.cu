@@ -481,7 +481,12 @@ bool eight_ok(const varco_norm_desc_t *d, const void *y8, const float *scales) {
 
 }  // namespace
 
-size_t vops::norm_scratch_bytes(int F) { return (size_t)max_parts(F) * F * 4; }
+// Lines for every width up to F: max_parts rounds down, so a narrower row can need some bytes more than F itself does (512
+// wide: 8 MB, 1000 wide: 8 MB - 608 bytes).
+size_t vops::norm_scratch_bytes(int F) {
+  const size_t most = (size_t)148 * 32 * F * 4, all = (size_t)8 << 20, least = (size_t)148 * 2 * F * 4;
+  return most < all ? most : least > all ? least : all;
+}
 
 extern "C" {
 
@@ -519,7 +524,7 @@ int varco_norm_bwd(const varco_norm_desc_t *d, const void *dY, const void *H, co
   unsigned *arrived = nullptr;
   if (dgain) {
     if (!workspace) return VARCO_INVALID_ARG;
-    if (ws_bytes < 256 + kStatusBytes + vops::norm_scratch_bytes(d->F)) return VARCO_WORKSPACE_TOO_SMALL;
+    if (ws_bytes < 256 + kStatusBytes + (size_t)max_parts(d->F) * d->F * 4) return VARCO_WORKSPACE_TOO_SMALL;
     arrived = reinterpret_cast<unsigned *>(ws_align(workspace) + 160);
     part = reinterpret_cast<float *>(ws_align(workspace) + kStatusBytes);
   }

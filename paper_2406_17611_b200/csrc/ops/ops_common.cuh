@@ -135,7 +135,7 @@ inline int sm_count() {
     return 0;
   return n;
 }
-size_t norm_scratch_bytes(int F);
+size_t norm_scratch_bytes(int F);         // of rows up to F wide
 size_t clip_scratch_bytes();
 
 }  // namespace vops

@@ -228,6 +228,21 @@ def test_gain_gradient_calls_in_a_row():
     assert vb.varco_workspace_status(ws) == 0
 
 
+@pytest.mark.parametrize("most", [445, 602, 640, 1000, 1536])
+def test_gain_gradient_in_the_workspace_of_wider_rows(most):
+    """A workspace for rows up to `most` wide serves every narrower one, with as many CTAs as the GPU takes.  Values pass fewer
+    additions than there are rows."""
+    g = gen(most)
+    ws = vb.varco_ops_workspace(most)
+    for F in (442, 443, 512, 600, most):
+        if F <= most:
+            H, DY = matrix(randn(20000, F, g), torch.bfloat16), matrix(randn(20000, F, g), torch.bfloat16)
+            rstd = torch.rand(20000, generator=g, device=DEV)
+            out = vb.varco_norm_bwd(DY, H, rstd, F, gain=torch.ones(F, device=DEV), workspace=ws).dgain
+            terms = d64(H, F) * d64(DY, F) * rstd.double()[:, None]
+            assert bool(((out.double() - terms.sum(0)).abs() <= 20002 * U * terms.abs().sum(0)).all())
+
+
 # ------------------------------------------------------------------------------------------ 8-bit forms
 @pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16], ids=["f32", "bf16"])
 @pytest.mark.parametrize("rows,F", [(1, 1), (2, 128), (7, 129), (1000, 47), (33, 602), (5, 5000)])

@@ -42,6 +42,20 @@ def test_workspace_sizes():
     assert L.varco_weight_grad_workspace_bytes(0, 256, C.byref(b)) == INVALID
 
 
+def test_workspace_covers_every_narrower_width():
+    """What is sized for F_max is passed with every width up to it, and a call at width F is content with the size for F."""
+    b = C.c_size_t()
+    L = vb.lib()
+    before = 0
+    for F in range(1, 16385):
+        assert L.varco_ops_workspace_bytes(F, C.byref(b)) == OK
+        assert b.value >= before, F
+        before = b.value
+    # the largest partials of the gain gradient: 4736 lines while they fit 8 MB, then as many lines as do, at least 296
+    assert L.varco_ops_workspace_bytes(602, C.byref(b)) == OK and b.value >= 512 + (8 << 20)
+    assert L.varco_ops_workspace_bytes(16384, C.byref(b)) == OK and b.value == 512 + 296 * 16384 * 4
+
+
 @pytest.mark.parametrize("change,want", [
     (dict(rows=-1), INVALID), (dict(F=0), INVALID), (dict(dtype=2), INVALID), (dict(eps=0.0), INVALID), (dict(eps=float("nan")), INVALID),
     (dict(F=16385), UNSUPPORTED), (dict(ldx=56), INVALID), (dict(ldx=65), INVALID), (dict(ldy=59), INVALID), (dict(lds=3), INVALID),
