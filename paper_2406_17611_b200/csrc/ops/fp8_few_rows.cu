@@ -54,6 +54,9 @@ __global__ void __launch_bounds__(kWarps * 32, few_rows_ctas(TILES * 8)) few_row
   constexpr int ROWS = TILES * 8;          // of A
   __shared__ float part[kWarps][ROWS][kCols + 1];
   __shared__ uint32_t amax[8][ROWS];       // of the cluster's CTAs
+  // Another CTA's shared memory may be written once that CTA has started: each says so here, and who writes waits for all eight
+  // behind its contraction.
+  if constexpr (QUANT) asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory");
   const int warp = threadIdx.x / 32, lane = threadIdx.x % 32, g = lane / 4, l = lane % 4;
   const int n0 = blockIdx.x * kCols;
   const uint8_t *b0 = p.b + (int64_t)min(n0 + g, p.N - 1) * p.ldb, *b1 = p.b + (int64_t)min(n0 + g + 8, p.N - 1) * p.ldb;
@@ -121,6 +124,8 @@ __global__ void __launch_bounds__(kWarps * 32, few_rows_ctas(TILES * 8)) few_row
   if constexpr (QUANT) {
     uint32_t rank;
     asm("mov.u32 %0, %%cluster_ctarank;" : "=r"(rank));
+    __syncwarp();
+    asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");   // pairs with the arrival at the start
 #pragma unroll
     for (int i = 0; i < PER; ++i) {
       const int m = threadIdx.x / kCols + i * (kWarps * 32 / kCols);

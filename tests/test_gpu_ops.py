@@ -347,6 +347,22 @@ def test_fp8_product_few_rows(M, N, K):
     test_fp8_product(M, N, K, torch.bfloat16)
 
 
+def test_few_rows_clusters_that_start_apart():
+    """The CTAs of a cluster exchange their rows' largest magnitudes.  Widths that leave a cluster's last CTAs without columns and
+    more clusters than run at once, launched back to back: every call gives the first one's scales and bytes, and these are right."""
+    g = gen(25)
+    ws = vb.varco_ops_workspace()
+    for M, N, K in ((1, 9400, 128), (8, 4096, 64), (20, 1040, 3000), (32, 130, 16), (5, 17, 1)):
+        A8, sA, a = operand(M, K, g)
+        B, b = weight(N, K, g)
+        outs = [vb.varco_fp8_product(A8, sA, B.data, B.scales, K, keep=False, quantize=True, workspace=ws) for _ in range(40)]
+        y = a @ b.t()
+        check_eight(outs[0].Y8, outs[0].scales, y, product_error(a, b, K) + 2 * U * y.abs())
+        for o in outs[1:]:
+            assert torch.equal(o.scales, outs[0].scales)
+            assert torch.equal(o.Y8.view(torch.uint8)[:, :N], outs[0].Y8.view(torch.uint8)[:, :N])
+
+
 def test_fp8_product_backward_is_the_adjoint():
     """<dY, A B^T> = <dY B, A> with the 8-bit forms of both sides: the transposed bytes and exchanged scale strides of a
     weight are the same matrix."""
