@@ -153,7 +153,7 @@ template <int PARTS, int ES>
 __device__ __forceinline__ void store_lines(const uint4 *stg, char *base, int64_t stride, int row0, int col, int M, int N, int lane) {
   constexpr int R = 32 / PARTS, V = 16 / ES;
   const int r0 = lane / PARTS, j = lane % PARTS;
-  char *out = base + (int64_t)(row0 + r0) * stride + (col + j * V) * ES;
+  char *out = base + (int64_t)(row0 + r0) * stride + (int64_t)(col + j * V) * ES;   // bytes: past 2^31 for wide outputs
   if (row0 + 32 <= M && col + PARTS * V <= N) {
     uint4 v[PARTS];
 #pragma unroll

@@ -47,3 +47,26 @@ def test_product_and_norm_past_31_bits():
     norm = vb.varco_clip_step([w], [gr], 1.0, 1e30, workspace=ws)
     assert abs(float(norm) - (0.25 * (ROWS * F - 1) + 16.0) ** 0.5) <= 2.0 ** -20 * float(norm)
     assert float(w[0]) == 0.5 and float(w[-1]) == -3.0 and float(w[-2]) == 0.5 and float(w[ROWS * F // 2]) == 0.5
+
+
+def test_product_of_more_than_two_gigabytes_a_row():
+    """One row of 600 million columns in fp32 with mask and 8-bit output: byte offsets inside the row pass 2^31, scale strides
+    too.  The columns around 2^29, where a 32-bit byte offset wraps, and both ends against 64 bits."""
+    N, K = 600_000_000, 16
+    g = gen(2)
+    ws = vb.varco_ops_workspace()
+    A = vb.varco_quantize_rows(torch.randn((1, K), generator=g, device="cuda:0"), K)
+    B = torch.randint(0, 0x7F, (N, K), generator=g, device="cuda:0", dtype=torch.uint8).view(torch.float8_e4m3fn)     # 0 to 448
+    sB = torch.rand(((N + 127) // 128, 1), generator=g, device="cuda:0") + 0.5
+    mask = torch.randn((1, N), generator=g, device="cuda:0")
+    out = vb.varco_fp8_product(A.data, A.scales, B, sB, K, mask=mask, dtype=torch.float32, quantize=True, workspace=ws)
+    assert vb.varco_workspace_status(ws) == 0
+    a = A.data.double() * A.scales.double()
+    for at in (0, (1 << 28) - 512, (1 << 29) - 512, (1 << 29) + 128 * 9999, N - N % 128 - 1024):
+        cols = torch.arange(at, min(at + 1024, N), device="cuda:0")
+        b = B[cols].double() * sB[cols // 128].double()
+        on = mask[:, cols] > 0
+        y = torch.where(on, a @ b.t(), 0.0)
+        e = torch.where(on, product_error(a, b, K) + 2 * U * y.abs(), 0.0)
+        assert bool(((out.Y[:, cols].double() - y).abs() <= e + 2 * U * y.abs()).all()), at
+        check_eight(out.Y8[:, cols], out.scales[at // 128:(int(cols[-1]) + 128) // 128].contiguous(), y, e)
