@@ -401,6 +401,13 @@ __global__ void __launch_bounds__(CFG::kThreads, CFG::CTAS) fp8_product_kernel(c
       }
       float inv = 0.f;
       if (p.y8) {
+        if (col0 + COLS > p.N) {
+          // Columns past N are scale x 0: NaN where the scale is not finite, and the mask has no say there.  They must not
+          // reach the block's magnitude: a row whose mask leaves nothing is zero whatever its operand holds.
+#pragma unroll
+          for (int i = 0; i < COLS / 2; ++i)
+            acc[i] = make_float2(col0 + 2 * i < p.N ? acc[i].x : 0.f, col0 + 2 * i + 1 < p.N ? acc[i].y : 0.f);
+        }
         float t0 = 0.f, t1 = 0.f, t2 = 0.f, t3 = 0.f;
 #pragma unroll
         for (int i = 0; i < COLS / 2; i += 4) {

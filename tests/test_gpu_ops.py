@@ -393,6 +393,39 @@ def test_fp8_product_infinite_and_nan_rows_stay_in_their_rows():
     assert bool(torch.isnan(out.Y[bad][:, :200].float()).all()) and bool(torch.isnan(out.scales[:, bad]).all())
 
 
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32], ids=["bf16", "f32"])
+@pytest.mark.parametrize("M,N,K", [(5, 41, 130), (30, 200, 64), (40, 41, 130), (40, 100, 64), (200, 70, 300), (40, 200, 64), (1000, 300, 64),
+                                   (20001, 100, 130), (9001, 531, 130)])
+def test_masked_rows_that_are_not_finite(M, N, K, dtype):
+    """A row of A with a NaN and one with an infinity, masked whole and in part: what the mask leaves out is zero, in both outputs,
+    whatever stands there; a mask's padding (here ones) is no mask.  All other rows are as without them."""
+    g = gen(M + N)
+    ws = vb.varco_ops_workspace()
+    x = randn(M, K, g)
+    x[1, 0], x[2, K - 1], x[3, 1], x[4, 2] = float("nan"), float("inf"), float("nan"), -float("inf")
+    A = vb.varco_quantize_rows(matrix(x, torch.float32), K)
+    B, b = weight(N, K, g)
+    u = randn(M, N, g)
+    u[1:3] = 0                                           # nothing is left of rows 1 and 2
+    u[3, :N - 1], u[3, N - 1] = -1, 1                    # the last column is left of row 3
+    out = vb.varco_fp8_product(A.data, A.scales, B.data, B.scales, K, mask=matrix(u, dtype, 1, fill=1.0), dtype=dtype, quantize=True,
+                               workspace=ws)
+    bad = [1, 2, 3, 4]
+    last = (N - 1) // 128 * 128                          # first column of the last block
+    assert not out.Y[1:3, :N].any() and not out.Y8[1:3, :N].view(torch.uint8).any()
+    assert bool((out.scales[:, 1:3] == 2.0 ** -126).all())
+    assert not out.Y[3, :N - 1].any() and bool(torch.isnan(out.Y[3, N - 1]))
+    v = out.Y8[:, :N].double() * spread(out.scales, N)
+    assert not v[3, :last].any() and bool(torch.isnan(v[3, last:N]).all())
+    good = torch.ones(M, dtype=torch.bool, device=DEV)
+    good[bad] = False
+    a = A.data[good].double()[:, :K] * spread(A.scales[:, good].contiguous(), K)
+    on = u.to(dtype)[good] > 0
+    y, e = torch.where(on, a @ b.t(), 0.0), torch.where(on, product_error(a, b, K) + 2 * U * (a @ b.t()).abs(), 0.0)
+    assert bool(((d64(out.Y[good], N) - y).abs() <= e + roundoff(dtype) * y.abs()).all())
+    check_eight(out.Y8[good], out.scales[:, good].contiguous(), y, e)
+
+
 def test_fp8_product_is_reproducible_and_empty():
     g = gen(23)
     ws = vb.varco_ops_workspace()
