@@ -1,7 +1,7 @@
-// Inline-PTX wrappers of the 5th-generation tensor-core path used by the 8-bit product: mbarriers with bounded waits,
-// TMA tile copies, TMEM allocation and loads, tcgen05.mma of kind f8f6f4, tensor maps.
-#ifndef VARCO_OPS_TC_CUH_
-#define VARCO_OPS_TC_CUH_
+// Inline-PTX wrappers of the 5th-generation tensor-core path: mbarriers with bounded waits, TMA tile copies, TMEM allocation
+// and loads, tcgen05.mma of kinds f16 and f8f6f4, descriptors, tensor maps.
+#ifndef VARCO_TC_CUH_
+#define VARCO_TC_CUH_
 
 #include <cuda.h>
 
@@ -81,6 +81,14 @@ __device__ __forceinline__ void tmem_dealloc(uint32_t taddr, uint32_t cols) {
 __device__ __forceinline__ void tc_fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
 __device__ __forceinline__ void tc_fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
 
+__device__ __forceinline__ void umma_bf16(uint32_t d_tmem, uint64_t adesc, uint64_t bdesc, uint32_t idesc, uint32_t accumulate) {
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t"
+      "setp.ne.b32 p, %4, 0;\n\t"
+      "tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}" ::"r"(d_tmem),
+      "l"(adesc), "l"(bdesc), "r"(idesc), "r"(accumulate)
+      : "memory");
+}
 __device__ __forceinline__ void umma_f8(uint32_t d_tmem, uint64_t adesc, uint64_t bdesc, uint32_t idesc, uint32_t accumulate) {
   asm volatile(
       "{\n\t.reg .pred p;\n\t"
@@ -119,16 +127,24 @@ template <int N> __device__ __forceinline__ void regs_inc() { asm volatile("setm
 template <int N> __device__ __forceinline__ void regs_dec() { asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(N)); }
 __device__ __forceinline__ void tmem_ld_wait() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
 
-// Shared-memory matrix descriptor of a K-major operand under the 128-byte swizzle: rows of 128 bytes, 8-row groups
-// 1024 bytes apart.
-__device__ __forceinline__ uint64_t smem_desc_kmajor(uint32_t saddr) {
+// Shared-memory matrix descriptor, 128-byte swizzle, Blackwell descriptor version 1.
+//   K-major operand : rows of 128 bytes, 8-row groups 1024 B apart (SBO); LBO unused (1).
+//   MN-major operand: rows are K indices holding 64 contiguous MN elements of 2 bytes; 8-row K groups 1024 B apart (SBO);
+//                     successive 64-element MN chunks `lbo_bytes` apart (LBO).
+__device__ __forceinline__ uint64_t smem_desc(uint32_t saddr, uint32_t lbo_bytes, uint32_t sbo_bytes) {
   uint64_t d = 0;
   d |= (uint64_t)((saddr & 0x3FFFFu) >> 4);
-  d |= 1ull << 16;                      // leading offset: unused in this layout
-  d |= (uint64_t)(1024 >> 4) << 32;     // stride between 8-row groups
-  d |= 1ull << 46;                      // descriptor version
-  d |= 2ull << 61;                      // SWIZZLE_128B
+  d |= (uint64_t)((lbo_bytes >> 4) & 0x3FFFu) << 16;
+  d |= (uint64_t)((sbo_bytes >> 4) & 0x3FFFu) << 32;
+  d |= 1ull << 46;   // descriptor version
+  d |= 2ull << 61;   // SWIZZLE_128B
   return d;
+}
+__device__ __forceinline__ uint64_t smem_desc_kmajor(uint32_t saddr) { return smem_desc(saddr, 16, 1024); }
+// Instruction descriptor of kind f16: bf16 inputs, 32-bit accumulation.
+__host__ __device__ constexpr uint32_t instr_desc_bf16(int M, int N, int a_mn_major, int b_mn_major) {
+  return (1u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)a_mn_major << 15) | ((uint32_t)b_mn_major << 16) |
+         ((uint32_t)(N >> 3) << 17) | ((uint32_t)(M >> 4) << 24);
 }
 // Instruction descriptor of kind f8f6f4: e4m3 inputs, 32-bit accumulation, both operands K-major.
 __host__ __device__ constexpr uint32_t instr_desc_e4m3(int M, int N) {
@@ -169,4 +185,4 @@ inline int make_map(CUtensorMap *m, const void *ptr, CUtensorMapDataType type, i
 
 }  // namespace vtc
 
-#endif  // VARCO_OPS_TC_CUH_
+#endif  // VARCO_TC_CUH_
