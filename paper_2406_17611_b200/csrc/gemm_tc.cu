@@ -18,8 +18,8 @@
 // 128-feature tiles and a contiguous range of nodes; fp32 partial results go to scratch and are
 // summed in a fixed order.
 //
-// Every mbarrier wait is bounded: on expiry the kernel raises an error flag in global memory,
-// every role leaves its loop, TMEM is released and the kernel returns.
+// Every mbarrier wait is bounded: on expiry the kernel raises an error flag in global memory, every role leaves its loop, loads and
+// instructions in flight are waited for (bounded as well), TMEM is released and the kernel returns.
 #include <cstring>
 
 #include "device_common.cuh"
@@ -68,7 +68,7 @@ struct RowsParams {
 };
 
 struct RowsSmem {
-  uint64_t full[kStagesRows], empty[kStagesRows], tfull[2], tempty[2];
+  uint64_t full[kStagesRows], empty[kStagesRows], tfull[2], tempty[2], drained;
   uint32_t tmem_base;
   int abort_flag;
   float bias[256];
@@ -96,6 +96,7 @@ __global__ void __launch_bounds__(kThreads, 1) rows_kernel(const __grid_constant
       mbar_init(&sh->tfull[a], 1);
       mbar_init(&sh->tempty[a], kEpiWarps);
     }
+    mbar_init(&sh->drained, 1);
     sh->abort_flag = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
@@ -132,12 +133,7 @@ __global__ void __launch_bounds__(kThreads, 1) rows_kernel(const __grid_constant
           }
         }
       }
-      if (!ok) {
-        // let loads that are still in flight land before the CTA retires
-        for (int s = 0; s < kStagesRows; ++s)
-          for (uint32_t it = 0; it < 4096u; ++it)
-            if (mbar_try_wait(&sh->full[s], 0) || mbar_try_wait(&sh->full[s], 1)) break;
-      }
+      drain_loads<kStagesRows>(sh->full, stage, phase);
     }
   } else if (warp == kMmaWarp) {
     if (lane == 0) {
@@ -174,6 +170,7 @@ __global__ void __launch_bounds__(kThreads, 1) rows_kernel(const __grid_constant
         }
         if (ok) umma_commit(&sh->tfull[acc]);
       }
+      drain_umma(&sh->drained);
     }
   } else {
     // epilogue warps: warp w reads TMEM lanes [32 (w % 4), + 32) = tile rows and takes every second
@@ -263,7 +260,7 @@ struct DwParams {
 };
 
 struct DwSmem {
-  uint64_t full[kStagesDw], empty[kStagesDw], done;
+  uint64_t full[kStagesDw], empty[kStagesDw], done, drained;
   uint32_t tmem_base;
   int abort_flag;
 };
@@ -286,6 +283,7 @@ __global__ void __launch_bounds__(kThreadsDw, 1) dw_kernel(const __grid_constant
       mbar_init(&sh->empty[s], 1);
     }
     mbar_init(&sh->done, 1);
+    mbar_init(&sh->drained, 1);
     sh->abort_flag = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
@@ -325,10 +323,7 @@ __global__ void __launch_bounds__(kThreadsDw, 1) dw_kernel(const __grid_constant
           phase ^= 1u;
         }
       }
-      if (!ok)
-        for (int s = 0; s < kStagesDw; ++s)
-          for (uint32_t it = 0; it < 4096u; ++it)
-            if (mbar_try_wait(&sh->full[s], 0) || mbar_try_wait(&sh->full[s], 1)) break;
+      drain_loads<kStagesDw>(sh->full, stage, phase);
     }
   } else if (warp == 5) {
     if (lane == 0) {
@@ -359,6 +354,7 @@ __global__ void __launch_bounds__(kThreadsDw, 1) dw_kernel(const __grid_constant
         }
       }
       if (ok) umma_commit(&sh->done);
+      drain_umma(&sh->drained);
     }
   } else {
     // epilogue: tile row = feature, 16 columns at a time, fp32 partials

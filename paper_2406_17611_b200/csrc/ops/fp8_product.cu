@@ -21,7 +21,8 @@
 // 170, add 450, hand back 100: 615 a block with two), not by the 512 clocks of instructions; and by the power cap (16,384 x
 // 4096 x 4096: 0.30 ms = 1.83 PFLOP/s in a burst, 0.34 ms sustained).
 // Every mbarrier wait is bounded: on expiry the status word is set, every role runs to its end without waiting (the
-// outputs are then invalid), TMEM is released and the kernel returns.
+// outputs are then invalid), loads and instructions in flight are waited for (bounded as well), TMEM is released and the
+// kernel returns.
 #include <cstring>
 
 #include "fp8_product.h"
@@ -66,7 +67,7 @@ template <int NT_, int EPI_, int STAGES_, int REGS_, int PIECES_, int CH_, int C
   static constexpr uint32_t kBias = kScales + ACCS * NB * kTileM * 4;
   static constexpr uint32_t kExch = kBias + EPI * kCols * 4;
   static constexpr uint32_t kBars = kExch + (kCols < kBlock && NT >= kBlock ? 2 * EPI * 32 * 4 : 0);
-  static constexpr uint32_t kTotal = kBars + (2 * STAGES + 2 * ACCS) * 8 + 16;
+  static constexpr uint32_t kTotal = kBars + (2 * STAGES + 2 * ACCS + 1) * 8 + 16;
   static constexpr int kLaunchRegs = 65536 / (CTAS * kThreads) / 8 * 8;
   static constexpr int kOtherRegs = (kLaunchRegs * kThreads - REGS * EPI * 32) / 128 / 8 * 8;
   static_assert(REGS == 0 || (kOtherRegs >= 24 && kOtherRegs * 128 + REGS * EPI * 32 <= kLaunchRegs * kThreads), "register split");
@@ -186,8 +187,8 @@ __global__ void __launch_bounds__(CFG::kThreads, CFG::CTAS) fp8_product_kernel(c
   uint8_t *base = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);
   uint8_t *sA = base, *sB = base + STAGES * CFG::kABytes;
   float *scales = reinterpret_cast<float *>(base + CFG::kScales);
-  uint64_t *full = reinterpret_cast<uint64_t *>(base + CFG::kBars), *empty = full + STAGES, *tfull = empty + STAGES, *tempty = tfull + ACCS;
-  uint32_t *tmem_slot = reinterpret_cast<uint32_t *>(tempty + ACCS);
+  uint64_t *full = reinterpret_cast<uint64_t *>(base + CFG::kBars), *empty = full + STAGES, *tfull = empty + STAGES, *tempty = tfull + ACCS, *drained = tempty + ACCS;
+  uint32_t *tmem_slot = reinterpret_cast<uint32_t *>(drained + 1);
   volatile int *abort_flag = reinterpret_cast<volatile int *>(tmem_slot + 1);
   const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
 
@@ -200,6 +201,7 @@ __global__ void __launch_bounds__(CFG::kThreads, CFG::CTAS) fp8_product_kernel(c
       mbar_init(&tfull[a], 3);          // the tensor cores' commit and the two scale warps
       mbar_init(&tempty[a], EPI);
     }
+    mbar_init(drained, 1);
     *abort_flag = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
@@ -231,10 +233,7 @@ __global__ void __launch_bounds__(CFG::kThreads, CFG::CTAS) fp8_product_kernel(c
           }
         }
       }
-      if (!ok)   // let loads that are still in flight land before the CTA retires
-        for (int s = 0; s < STAGES; ++s)
-          for (uint32_t it = 0; it < 4096u; ++it)
-            if (mbar_try_wait(&full[s], 0) || mbar_try_wait(&full[s], 1)) break;
+      drain_loads<STAGES>(full, stage, phase);
     } else if (warp == EPI + 1 && lane == 0) {
       const uint32_t idesc = instr_desc_e4m3(kTileM, NT);
       int stage = 0;
@@ -261,6 +260,7 @@ __global__ void __launch_bounds__(CFG::kThreads, CFG::CTAS) fp8_product_kernel(c
           }
         }
       }
+      drain_umma(drained);
     } else if (warp >= EPI + 2) {
       // rows r0 and r0 + 32 of the tile: sA of the row times sB of each 128-column block
       const int r0 = (warp - EPI - 2) * 64 + lane, M = (int)p.M;

@@ -63,6 +63,20 @@ __device__ __forceinline__ bool mbar_wait(uint64_t *bar, uint32_t parity, volati
   return false;
 }
 
+// Wait of a role that is about to leave: bounded too, but raises nothing (who gave up has said so).
+__device__ __forceinline__ void mbar_wait_quietly(uint64_t *bar, uint32_t parity) {
+  const long long t0 = clock64();
+  while (!mbar_try_wait<kIdleNs>(bar, parity) && clock64() - t0 <= kSpinClocks) {
+  }
+}
+// Parity of the phase that stage s's last fill completes, for a loader that would fill `stage` next with parity `phase`.  A stage
+// that was never filled gives the phase before the first, which every wait takes as complete.
+__host__ __device__ constexpr uint32_t last_fill(int s, int stage, uint32_t phase) { return s < stage ? phase : phase ^ 1u; }
+// Every load that the loader has issued has landed: before that its CTA must not retire, whoever gave up.
+template <int STAGES> __device__ __forceinline__ void drain_loads(uint64_t *full, int stage, uint32_t phase) {
+  for (int s = 0; s < STAGES; ++s) mbar_wait_quietly(&full[s], last_fill(s, stage, phase));
+}
+
 __device__ __forceinline__ void tma_load_2d(void *smem_dst, const CUtensorMap *tmap, int x, int y, uint64_t *bar) {
   asm volatile(
       "cp.async.bulk.tensor.2d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];" ::"r"(
@@ -101,6 +115,12 @@ __device__ __forceinline__ void umma_f8(uint32_t d_tmem, uint64_t adesc, uint64_
 __device__ __forceinline__ void umma_commit(uint64_t *bar) {
   asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(smem_u32(bar))
                : "memory");
+}
+// Every tcgen05.mma that this thread has issued has completed, whoever gave up: before that TMEM must not be freed and the
+// operands' shared memory not left.  `drained`: a barrier of its own with a count of one.
+__device__ __forceinline__ void drain_umma(uint64_t *drained) {
+  umma_commit(drained);
+  mbar_wait_quietly(drained, 0);
 }
 // 16 or 32 accumulator columns of this thread's TMEM lane
 __device__ __forceinline__ void tmem_ld(uint32_t taddr, float2 (&r)[8]) {
