@@ -92,7 +92,11 @@ int64_t matrix(const Tensor &t, const char *what, int64_t rows, int64_t F, Scala
   TORCH_CHECK_TYPE(dtype == ScalarType::Undefined || t.scalar_type() == dtype, what, " must be ", dtype, ", not ", t.scalar_type());
   TORCH_CHECK_VALUE((rows < 0 || t.size(0) == rows) && t.size(1) >= F, what, " is [", t.size(0), " x ", t.size(1), "]: ",
                     rows < 0 ? "any number of" : std::to_string(rows), " rows and at least ", F, " columns are wanted");
-  return t.size(0) > 1 ? t.stride(0) : t.size(1);   // torch reports any stride for a single row
+  if (t.size(0) > 1) return t.stride(0);
+  // A single row has no stride of its own and torch reports any number.  Where it is one that rows could have (a row out of a
+  // padded matrix), it tells that the padding is there; else the row ends with its columns.
+  const int64_t ld = t.stride(0), vec = 16 / (int64_t)t.element_size();
+  return ld >= t.size(1) && ld % vec == 0 ? ld : t.size(1);
 }
 const float *vector(const Tensor &t, const char *what, int64_t n, c10::Device dev) {
   TORCH_CHECK_TYPE(t.scalar_type() == at::kFloat, what, " must be float32");

@@ -466,6 +466,38 @@ def test_weight_grad(rows, Fa, Fb, dtype):
     assert vb.varco_workspace_status(ws) == 0
 
 
+# ------------------------------------------------------------------------------------------ slices of rows
+@pytest.mark.parametrize("n", [1, 2, 5])
+def test_slices_of_padded_matrices_with_any_number_of_rows(n):
+    """The first n rows and the columns in use of padded matrices, as a caller slices them: one row is taken as several are, and
+    gives what it gives among them."""
+    g = gen(31)
+    ws, gws, G = vb.varco_ops_workspace(60), vb.varco_weight_grad_workspace(60, 60), torch.ones(60, device=DEV)
+    cut = lambda t, F=60: t[:n, :F]  # noqa: E731
+    same = lambda a, b, F=60: torch.equal(a[:, :F].contiguous().view(torch.uint8), b[:n, :F].contiguous().view(torch.uint8))  # noqa: E731
+    M = matrix(randn(5, 60, g), torch.bfloat16)
+    all_, some = (vb.varco_norm_fwd(x, 60, gain=G, residual=x, quantize=True) for x in (M, cut(M)))
+    assert same(some.Y, all_.Y) and same(some.H, all_.H) and same(some.Y8, all_.Y8) and torch.equal(some.scales, all_.scales[:, :n])
+    back = [vb.varco_norm_bwd(f(M), f(all_.H), f(all_.rstd[:, None], 1)[:, 0].contiguous(), 60, gain=G, residual_grad=f(M), workspace=ws).dX
+            for f in (lambda t, F=60: t, cut)]
+    assert same(back[1], back[0])
+    e = vb.varco_quantize_rows(cut(M), 60)
+    W = vb.varco_quantize_weight(torch.randn((20, 60), generator=g, device=DEV))
+    mask = matrix(randn(5, 20, g), torch.bfloat16)
+    p = [vb.varco_fp8_product(f(a), s, W.data[:, :60], W.scales, 60, mask=f(mask, 20), workspace=ws).Y
+         for f, a, s in ((lambda t, F=60: t[:, :F], vb.varco_quantize_rows(M, 60).data, vb.varco_quantize_rows(M, 60).scales), (cut, e.data, e.scales))]
+    assert same(p[1], p[0], 20)
+    dW, _ = vb.varco_weight_grad(cut(M), 60, cut(M), 60, gws)
+    a = d64(M, 60)[:n]
+    assert bool(((dW.double() - a.t() @ a).abs() <= 2 * (n + 1) * U * (a.abs().t() @ a.abs())).all())
+
+
+def test_a_single_row_that_ends_with_its_columns_is_refused_as_several_are():
+    for n in (1, 2):
+        with pytest.raises(vb.VarcoError):
+            vb.varco_norm_fwd(torch.zeros((n, 60), dtype=torch.bfloat16, device=DEV), 60)
+
+
 # ------------------------------------------------------------------------------------------ refusals
 def test_refusals():
     X = torch.zeros((4, 64), dtype=torch.bfloat16, device=DEV)
