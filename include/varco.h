@@ -286,6 +286,9 @@ int varco_workspace_status(const void *workspace, void *stream, int *device_stat
  *                              column block b is scales[b * lds + m], lds >= rows
  *   weights                    one scale per 128 x 128 block
  *
+ * Padding.  An output's columns past the last one in use are written as zero up to the next 16 bytes, whatever its row holds;
+ * columns behind them are left alone.  An input's padding may hold anything.
+ *
  * Workspace.  Operators that take one want varco_ops_workspace_bytes bytes of device memory, zeroed once by the caller
  * before its first use and then passed to any number of calls, as long as these follow each other on one stream.
  * varco_workspace_status reads its status word: 0 = no call since it was zeroed gave up on a bounded wait.
@@ -301,8 +304,7 @@ int varco_ops_workspace_bytes(int32_t F_max, size_t *bytes);
  *   H, rstd from the forward; dRes NULL = 0.  dX is the gradient of both addends.  Outputs, each may be NULL: dX, dX8 +
  *   scales, dgain [F] fp32 (needs the workspace; summed in a fixed order).
  *   Descriptor: leading dimensions in elements.  ldx: X / dX, ldr: R / dRes, ldh: H, ldy: Y / dY, ld8: Y8 / dX8,
- *   lds: scales.  Those of absent matrices are ignored.  Columns [F, round_up(F, 16 bytes)) of outputs are written as
- *   zero.  eps > 0.  Errors: INVALID_ARG, WORKSPACE_TOO_SMALL, UNSUPPORTED (F > 16384), CUDA. */
+ *   lds: scales.  Those of absent matrices are ignored.  eps > 0.  Errors: INVALID_ARG, WORKSPACE_TOO_SMALL, UNSUPPORTED (F > 16384), CUDA. */
 typedef struct {
   int64_t rows;
   int32_t F;
@@ -319,7 +321,7 @@ int varco_norm_bwd(const varco_norm_desc_t *desc, const void *dY, const void *H,
 /* varco_quantize_rows     the 8-bit form of X [rows x F] with row-block scales.
  * varco_quantize_weight   the 8-bit form of W [rows x cols] (ldw in elements, any alignment of the element) with 128 x 128
  *   scales [ceil(rows/128) x lds], lds >= ceil(cols/128): W8 [rows x ld8] and WT8 [cols x ldt8] (the transposed bytes;
- *   same scales with the two indexes exchanged).  Either may be NULL.  Padding columns are written as zero. */
+ *   same scales with the two indexes exchanged).  Either may be NULL. */
 int varco_quantize_rows(int64_t rows, int32_t F, varco_dtype_t dtype, const void *X, int64_t ldx, void *Y8, int64_t ld8,
                         float *scales, int64_t lds, void *stream);
 int varco_quantize_weight(int32_t rows, int32_t cols, varco_dtype_t dtype, const void *W, int64_t ldw, void *W8, int64_t ld8,

@@ -105,6 +105,8 @@ __global__ void __launch_bounds__(kWarps * 32, few_rows_ctas(TILES * 8)) few_row
   constexpr int PER = (ROWS * kCols + kWarps * 32 - 1) / (kWarps * 32);
   float v[PER];
   const int c = threadIdx.x % kCols, n = n0 + c;
+  constexpr int V = ElemTraits<T>::kVec;
+  const int end = (p.N + V - 1) / V * V, end8 = (p.N + 15) / 16 * 16;     // columns with their padding, which becomes zero
 #pragma unroll
   for (int i = 0; i < PER; ++i) {
     const int m = threadIdx.x / kCols + i * (kWarps * 32 / kCols);
@@ -118,7 +120,7 @@ __global__ void __launch_bounds__(kWarps * 32, few_rows_ctas(TILES * 8)) few_row
     if (here && p.bias) r += p.bias[n];
     if (relu_on) r = relu(r);
     if (here && p.mask) r = ElemTraits<T>::to_f(((const T *)p.mask)[(int64_t)m * p.ldmask + n]) > 0.f ? r : 0.f;
-    if (here && p.y) ((T *)p.y)[(int64_t)m * p.ldy + n] = ElemTraits<T>::from_f(r);
+    if (m < p.M && n < end && p.y) ((T *)p.y)[(int64_t)m * p.ldy + n] = ElemTraits<T>::from_f(r);
     v[i] = r;
   }
   if constexpr (QUANT) {
@@ -141,12 +143,12 @@ __global__ void __launch_bounds__(kWarps * 32, few_rows_ctas(TILES * 8)) few_row
 #pragma unroll
     for (int i = 0; i < PER; ++i) {
       const int m = threadIdx.x / kCols + i * (kWarps * 32 / kCols);
-      if (m < p.M && m < ROWS && n < p.N) {
+      if (m < p.M && m < ROWS && n < end8) {
         uint32_t top = 0;
 #pragma unroll
         for (int r = 0; r < 8; ++r) top = max(top, amax[r][m]);
         const Scale s = block_scale(top);
-        p.y8[(int64_t)m * p.ldy8 + n] = (uint8_t)pack_e4m3x2(v[i] * s.inv, 0.f);
+        p.y8[(int64_t)m * p.ldy8 + n] = n < p.N ? (uint8_t)pack_e4m3x2(v[i] * s.inv, 0.f) : (uint8_t)0;
         if (rank == 0 && c == 0) p.sy[(int64_t)(n / kBlock) * p.ld_sy + m] = s.s;
       }
     }

@@ -61,7 +61,15 @@ __device__ __forceinline__ void store_e4m3(uint8_t *p, const float (&f)[8], floa
   *reinterpret_cast<uint2 *>(p) = make_uint2(pack_e4m3x4_scaled(f, inv), pack_e4m3x4_scaled(f + 4, inv));
 }
 
-// A row is worked on by a team of TEAM threads: 8, 16 or 32 lanes of a warp, or a whole CTA of TEAM threads.
+// An 8-bit row ends on a 16-byte boundary, its last chunk of V bytes may end before it: zeros up to there.
+template <int V> __device__ __forceinline__ void zero_to_boundary(uint8_t *row, int chunks) {
+  for (int b = chunks * V; b % 16; b += V) {
+    if (V == 4) *reinterpret_cast<uint32_t *>(row + b) = 0u;
+    else *reinterpret_cast<uint2 *>(row + b) = make_uint2(0u, 0u);
+  }
+}
+
+// A row is worked on by a team of TEAM threads: 2 to 32 lanes of a warp, or a whole CTA of TEAM threads.
 // Lane `l` holds the 16-byte chunks l, l + TEAM, ...: neighbouring lanes read neighbouring chunks.
 template <int TEAM> constexpr int threads_per_cta() { return TEAM <= 32 ? 256 : TEAM; }
 template <int TEAM> constexpr int rows_per_cta() { return threads_per_cta<TEAM>() / TEAM; }
@@ -105,14 +113,6 @@ template <int V> __device__ __forceinline__ void clear_padding(float (&f)[V], in
     for (int i = 0; i < V; ++i)
       if (c * V + i >= F) f[i] = 0.f;
   }
-}
-
-// 16 bytes of a row as floats; elements from column F on are padding and read as zero
-template <typename T, int V>
-__device__ __forceinline__ void load_chunk(const T *row, int c, int F, float (&f)[V]) {
-  const uint4 v = *reinterpret_cast<const uint4 *>(row + (int64_t)c * V);
-  unpack16(v, f, T());
-  clear_padding<V>(f, c, F);
 }
 
 // Entry-point checks: a matrix of `rows` x F elements of `es` bytes under the library's rule for activations.

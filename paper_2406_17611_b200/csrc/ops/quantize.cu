@@ -19,7 +19,8 @@ __global__ void __launch_bounds__(256) quantize_rows_kernel(const T *__restrict_
                                                             int64_t lds) {
   constexpr int V = ElemTraits<T>::kVec, LANES = kBlock / V, GROUPS = 256 / LANES, R = 4;   // R rows on their way
   const int lane = threadIdx.x % LANES, b = blockIdx.y, c = b * LANES + lane;
-  const bool col = c * V < F;
+  const int chunks = (F + V - 1) / V;
+  const bool col = c < chunks;
   const int64_t step = (int64_t)gridDim.x * GROUPS;
   // groups of one CTA take the same number of trips: those past the last row stay for the shuffles
   for (int64_t row0 = (int64_t)blockIdx.x * GROUPS; row0 < rows; row0 += step * R) {
@@ -42,17 +43,19 @@ __global__ void __launch_bounds__(256) quantize_rows_kernel(const T *__restrict_
       const Scale s = block_scale(lanes_max<LANES>(m));
       if (row < rows) {
         if (col) store_e4m3(Y8 + row * ld8 + (int64_t)c * V, f, s.inv);
+        if (c == chunks - 1) zero_to_boundary<V>(Y8 + row * ld8, chunks);
         if (lane == 0) scales[(int64_t)b * lds + row] = s.s;
       }
     }
   }
 }
 
-// One CTA per 128 x 128 block: a thread holds four neighbouring columns of 16 rows.
+// One CTA per 128 x 128 block: a thread holds four neighbouring columns of 16 rows.  `end` and `endt`: columns of W8 and of the
+// transposed bytes with their padding, multiples of 16.
 template <typename T>
 __global__ void __launch_bounds__(256) quantize_weight_kernel(const T *__restrict__ W, int64_t ldw, int R, int C,
-                                                              uint8_t *__restrict__ W8, int64_t ld8, uint8_t *__restrict__ T8,
-                                                              int64_t ldt8, float *__restrict__ scales, int64_t lds) {
+                                                              uint8_t *__restrict__ W8, int64_t ld8, int64_t end,
+                                                              uint8_t *__restrict__ T8, int64_t ldt8, int64_t endt, float *__restrict__ scales, int64_t lds) {
   __shared__ uint32_t tile[kBlock][kBlock / 4 + 1];
   __shared__ uint32_t amax[8];
   const int r0 = blockIdx.y * kBlock, c0 = blockIdx.x * kBlock;
@@ -84,8 +87,8 @@ __global__ void __launch_bounds__(256) quantize_weight_kernel(const T *__restric
     const int r = r0 + y + 8 * i;
     const uint32_t q = pack_e4m3x4_scaled(f[i], s.inv);
     tile[y + 8 * i][x] = q;
-    // row strides are multiples of 16: a group of four bytes is inside or outside as a whole
-    if (W8 && r < R && c0 + 4 * x < ld8) *reinterpret_cast<uint32_t *>(W8 + (int64_t)r * ld8 + c0 + 4 * x) = q;
+    // a group of four bytes is inside or outside as a whole
+    if (W8 && r < R && c0 + 4 * x < end) *reinterpret_cast<uint32_t *>(W8 + (int64_t)r * ld8 + c0 + 4 * x) = q;
   }
   __syncthreads();
   if (T8) {
@@ -94,7 +97,7 @@ __global__ void __launch_bounds__(256) quantize_weight_kernel(const T *__restric
 #pragma unroll 4
     for (int i = 0; i < 16; ++i) {
       const int c = y + 8 * i;           // column of the block, row of the transposed matrix
-      if (c0 + c < C && r0 + 4 * x < ldt8) {
+      if (c0 + c < C && r0 + 4 * x < endt) {
         uint32_t q = 0;
 #pragma unroll
         for (int j = 0; j < 4; ++j) q |= (uint32_t)bytes[(4 * x + j) * LD + c] << (8 * j);
@@ -135,10 +138,11 @@ int varco_quantize_weight(int32_t rows, int32_t cols, varco_dtype_t dtype, const
   const dim3 grid((cols + kBlock - 1) / kBlock, (rows + kBlock - 1) / kBlock);
   if (grid.y > 65535) return VARCO_UNSUPPORTED;
   cudaStream_t st = (cudaStream_t)stream;
+  const int64_t end = round_up64(cols, 16), endt = round_up64(rows, 16);
   if (dtype == VARCO_F32)
-    quantize_weight_kernel<float><<<grid, 256, 0, st>>>((const float *)W, ldw, rows, cols, (uint8_t *)W8, ld8, (uint8_t *)WT8, ldt8, scales, lds);
+    quantize_weight_kernel<float><<<grid, 256, 0, st>>>((const float *)W, ldw, rows, cols, (uint8_t *)W8, ld8, end, (uint8_t *)WT8, ldt8, endt, scales, lds);
   else
-    quantize_weight_kernel<__nv_bfloat16><<<grid, 256, 0, st>>>((const __nv_bfloat16 *)W, ldw, rows, cols, (uint8_t *)W8, ld8, (uint8_t *)WT8, ldt8, scales, lds);
+    quantize_weight_kernel<__nv_bfloat16><<<grid, 256, 0, st>>>((const __nv_bfloat16 *)W, ldw, rows, cols, (uint8_t *)W8, ld8, end, (uint8_t *)WT8, ldt8, endt, scales, lds);
   VARCO_KERNEL_LAUNCHED();
   return VARCO_OK;
 }

@@ -466,6 +466,63 @@ def test_weight_grad(rows, Fa, Fb, dtype):
     assert vb.varco_workspace_status(ws) == 0
 
 
+# ------------------------------------------------------------------------------------------ padding of outputs
+def garbage(rows, ld, dtype):
+    return torch.full((rows, ld * torch.empty((), dtype=dtype).element_size()), 0x7F, dtype=torch.uint8, device=DEV).view(dtype)
+
+
+def check_padding(t, F):
+    """Zero from column F to the next 16 bytes, untouched from there."""
+    es = t.element_size()
+    b, end = t.view(torch.uint8), ld_of(F, t.dtype) * es
+    assert not b[:, F * es:end].any() and bool((b[:, end:] == 0x7F).all())
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16], ids=["f32", "bf16"])
+@pytest.mark.parametrize("F", [1, 3, 4, 5, 8, 9, 15, 16, 17, 20, 127, 129, 300, 602, 1001, 4100])
+def test_padding_of_outputs(F, dtype):
+    """Outputs wider than their rows, full of bytes that are neither zero nor finite e4m3 values, at the C ABI; among the rows a
+    NaN and an infinity, whose scales are not finite."""
+    g, L, st = gen(F), vb.lib(), torch.cuda.current_stream().cuda_stream
+    dt, rows = vb.F32 if dtype == torch.float32 else vb.BF16, 37
+    x = randn(rows, F, g)
+    x[3, 0], x[5, F - 1] = float("nan"), float("inf")
+    X = matrix(x, dtype)
+    G, ws = torch.ones(F, device=DEV), vb.varco_ops_workspace(F)
+    P = lambda t: t.data_ptr()  # noqa: E731
+    ld, ld8, nb = ld_of(F, dtype, 3), ld_of(F, E4M3, 3), (F + 127) // 128
+    H, Y, Y8 = garbage(rows, ld, dtype), garbage(rows, ld, dtype), garbage(rows, ld8, E4M3)
+    s, rstd, dg = torch.empty((nb, rows), device=DEV), torch.empty(rows, device=DEV), torch.empty(F, device=DEV)
+    d = vb.NormDesc(rows, F, dt, 1e-6, X.shape[1], X.shape[1], ld, ld, ld8, rows)
+    assert L.varco_norm_fwd(d, P(X), P(X), P(G), P(H), P(Y), P(Y8), P(s), P(rstd), st) == 0
+    for t in (H, Y, Y8):
+        check_padding(t, F)
+    dX, dX8 = garbage(rows, ld, dtype), garbage(rows, ld8, E4M3)
+    d = vb.NormDesc(rows, F, dt, 1e-6, ld, X.shape[1], X.shape[1], X.shape[1], ld8, rows)
+    assert L.varco_norm_bwd(d, P(X), P(X), P(rstd), P(G), P(X), P(dX), P(dX8), P(s), P(dg), P(ws), ws.numel(), st) == 0
+    check_padding(dX, F), check_padding(dX8, F)
+    Y8 = garbage(rows, ld8, E4M3)
+    assert L.varco_quantize_rows(rows, F, dt, P(X), X.shape[1], P(Y8), ld8, P(s), rows, st) == 0
+    check_padding(Y8, F)
+    W8, T8, sw = garbage(rows, ld8, E4M3), garbage(F, ld_of(rows, E4M3, 20), E4M3), torch.empty((1, nb), device=DEV)
+    assert L.varco_quantize_weight(rows, F, dt, P(X), X.shape[1], P(W8), ld8, P(T8), T8.shape[1], P(sw), nb, st) == 0
+    check_padding(W8, F), check_padding(T8, rows)
+    # products of few rows and of many (tiles), F columns out: the weight's transposed bytes, 37 in use, as B
+    B, b = weight(F, rows, g)
+    for M in (1, 7, 30, 37, 300):
+        a = randn(M, rows, g)
+        a[M // 2, 0] = float("nan")
+        A = vb.varco_quantize_rows(matrix(a, torch.float32), rows)
+        Y, Y8, s = garbage(M, ld, dtype), garbage(M, ld8, E4M3), torch.empty((nb, M), device=DEV)
+        c = torch.randn(F, generator=g, device=DEV)
+        d = vb.Fp8Desc(M, F, rows, dt, 0, A.data.shape[1], B.data.shape[1], M, 1, 1, 0, ld, ld8, M)
+        assert L.varco_fp8_product(d, P(A.data), P(A.scales), P(B.data), P(B.scales), P(c), 0, P(Y), P(Y8), P(s), P(ws), ws.numel(), st) == 0
+        check_padding(Y, F), check_padding(Y8, F)
+        Y = garbage(M, ld, dtype)
+        assert L.varco_fp8_product(d, P(A.data), P(A.scales), P(B.data), P(B.scales), P(c), 0, P(Y), 0, 0, P(ws), ws.numel(), st) == 0
+        check_padding(Y, F)
+
+
 # ------------------------------------------------------------------------------------------ slices of rows
 @pytest.mark.parametrize("n", [1, 2, 5])
 def test_slices_of_padded_matrices_with_any_number_of_rows(n):
