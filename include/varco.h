@@ -291,7 +291,8 @@ int varco_workspace_status(const void *workspace, void *stream, int *device_stat
  *
  * Workspace.  Operators that take one want varco_ops_workspace_bytes bytes of device memory, zeroed once by the caller
  * before its first use and then passed to any number of calls, as long as these follow each other on one stream.
- * varco_workspace_status reads its status word: 0 = no call since it was zeroed gave up on a bounded wait.
+ * varco_workspace_status reads its status word: 0 = no call since it was zeroed gave up on a bounded wait (a second or so).
+ * The outputs of a call that gave up are not valid, and the workspace has to be zeroed again before the next.
  */
 /* Bytes that varco_norm_bwd (widths up to F_max), varco_fp8_product, varco_grad_norm, varco_grad_clip and
  * varco_clip_step need.  UNSUPPORTED beyond F_max = 16384. */

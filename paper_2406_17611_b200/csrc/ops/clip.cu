@@ -28,7 +28,7 @@ constexpr int kThreads = 256;
 constexpr int kMaxCtas = 148 * 8;          // partials of one group of tensors
 constexpr int kGroup = 800;                // tensors of the largest table: 32,000 bytes of parameters
 constexpr int kMaxGroups = 21;             // 16,800 tensors
-constexpr uint32_t kSpinLimit = 1u << 24;
+constexpr long long kSpinClocks = 2000000000ll;   // about one second of SM clocks
 
 enum Mode { kNorm = 0, kClip = 1, kStep = 2 };
 enum Pass { kBoth = 0, kPartials = 1, kApply = 2 };
@@ -121,7 +121,8 @@ template <typename T> __device__ double chunk_squares(const T *src, int n) {
 }
 
 // All CTAs of the grid have written what they wrote before it.  Bounded: false (and the status word set) when the others do
-// not come, which a cooperative launch rules out.
+// not come within a second, which a cooperative launch rules out as long as the counters are what the last call left: a
+// workspace that was not zeroed, or whose call gave up, has to be zeroed (again).
 __device__ bool grid_barrier(unsigned *bar, int *err) {
   __shared__ int ok;
   __syncthreads();
@@ -135,11 +136,14 @@ __device__ bool grid_barrier(unsigned *bar, int *err) {
       __threadfence();
       *gen = g + 1;
     } else {
-      uint32_t it = 0;
-      while (*gen == g && ++it < kSpinLimit) __nanosleep(32);
-      if (it >= kSpinLimit) {
-        ok = 0;
-        atomicCAS(err, 0, 31);
+      const long long t0 = clock64();
+      while (*gen == g) {
+        if (clock64() - t0 > kSpinClocks) {
+          ok = 0;
+          atomicCAS(err, 0, 31);
+          break;
+        }
+        __nanosleep(32);
       }
     }
     __threadfence();

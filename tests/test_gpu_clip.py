@@ -106,6 +106,24 @@ def test_reproducible():
     assert torch.equal(vb.varco_grad_norm(g, ws), vb.varco_grad_norm(g, ws))
 
 
+def test_a_barrier_that_the_others_never_reach_ends():
+    """Counters that no number of arrivals completes: the wait runs out after its second, the status says so, weights and norm stay
+    as they were, and the workspace works again once it is zeroed."""
+    ws = vb.varco_ops_workspace()
+    word = (-ws.data_ptr()) % 256 // 4 + 32               # of the aligned base: status at 0, barrier at 128 bytes
+    w, g = torch.ones(100000, device=DEV), torch.ones(100000, device=DEV)
+    ws[:1024].view(torch.int32)[word] = 1 << 30
+    start, end = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
+    start.record()
+    vb.varco_clip_step([w], [g], 0.5, 1e9, workspace=ws)
+    end.record()
+    assert vb.varco_workspace_status(ws) == 31
+    assert bool((w == 1).all()) and 500 < start.elapsed_time(end) < 5000
+    ws.zero_()
+    assert abs(float(vb.varco_clip_step([w], [g], 0.5, 1e9, workspace=ws)) - 100000 ** 0.5) <= 2.0 ** -20 * 100000 ** 0.5
+    assert bool((w == 0.5).all()) and vb.varco_workspace_status(ws) == 0
+
+
 def test_refusals():
     ws = vb.varco_ops_workspace()
     t, bad = torch.ones(64, device=DEV), pytest.raises((ValueError, TypeError, vb.VarcoError))
