@@ -52,8 +52,7 @@ __device__ __forceinline__ void quantize_row(const NormParams &p, int64_t row, i
     for (int j = j0; j < j0 + JB && j < NCH; ++j) {
       const int c = lane + j * TEAM;
       if (row < p.rows && c < nchunks) {
-        store_e4m3(p.y8 + row * p.ld8 + (int64_t)c * V, f[j], s.inv);
-        if (c == nchunks - 1) zero_to_boundary<V>(p.y8 + row * p.ld8, nchunks);
+        store_e4m3<V>(p.y8 + row * p.ld8, c, p.F, f[j], s.inv);
         if (c % PER == 0) p.scales[(int64_t)(c / PER) * p.lds + row] = s.s;
       }
     }

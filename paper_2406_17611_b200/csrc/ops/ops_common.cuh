@@ -54,18 +54,24 @@ __device__ __forceinline__ uint32_t pack_e4m3x4_scaled(float2 a, float2 b, float
 __device__ __forceinline__ uint32_t pack_e4m3x4_scaled(const float *f, float inv) {
   return pack_e4m3x4_scaled(make_float2(f[0], f[1]), make_float2(f[2], f[3]), inv);
 }
-__device__ __forceinline__ void store_e4m3(uint8_t *p, const float (&f)[4], float inv) {
-  *reinterpret_cast<uint32_t *>(p) = pack_e4m3x4_scaled(f, inv);
-}
-__device__ __forceinline__ void store_e4m3(uint8_t *p, const float (&f)[8], float inv) {
-  *reinterpret_cast<uint2 *>(p) = make_uint2(pack_e4m3x4_scaled(f, inv), pack_e4m3x4_scaled(f + 4, inv));
-}
-
-// An 8-bit row ends on a 16-byte boundary, its last chunk of V bytes may end before it: zeros up to there.
-template <int V> __device__ __forceinline__ void zero_to_boundary(uint8_t *row, int chunks) {
-  for (int b = chunks * V; b % 16; b += V) {
-    if (V == 4) *reinterpret_cast<uint32_t *>(row + b) = 0u;
-    else *reinterpret_cast<uint2 *>(row + b) = make_uint2(0u, 0u);
+// the first n bytes of a word, zeros behind them
+__device__ __forceinline__ uint32_t keep_bytes(uint32_t v, int n) { return n >= 4 ? v : n <= 0 ? 0u : v & ((1u << 8 * n) - 1u); }
+// Chunk c of a row of F columns in 8 bits, V columns a chunk.  What lies past F is zero, whatever the scale (a row's scale may be
+// NaN), and the last chunk takes the row to its next 16 bytes.
+template <int V> __device__ __forceinline__ void store_e4m3(uint8_t *row, int c, int F, const float (&f)[V], float inv) {
+  uint32_t w[V / 4];
+#pragma unroll
+  for (int i = 0; i < V / 4; ++i) w[i] = pack_e4m3x4_scaled(f + 4 * i, inv);
+  uint8_t *p = row + (int64_t)c * V;
+  const int left = F - c * V;
+  if (left < V) {
+#pragma unroll
+    for (int i = 0; i < V / 4; ++i) w[i] = keep_bytes(w[i], left - 4 * i);
+  }
+  if (V == 4) *reinterpret_cast<uint32_t *>(p) = w[0];
+  else *reinterpret_cast<uint2 *>(p) = make_uint2(w[0], w[V / 4 - 1]);
+  if (left <= V) {
+    for (int b = c * V + V; b % 16; b += 4) *reinterpret_cast<uint32_t *>(row + b) = 0u;
   }
 }
 

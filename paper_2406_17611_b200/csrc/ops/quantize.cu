@@ -19,8 +19,7 @@ __global__ void __launch_bounds__(256) quantize_rows_kernel(const T *__restrict_
                                                             int64_t lds) {
   constexpr int V = ElemTraits<T>::kVec, LANES = kBlock / V, GROUPS = 256 / LANES, R = 4;   // R rows on their way
   const int lane = threadIdx.x % LANES, b = blockIdx.y, c = b * LANES + lane;
-  const int chunks = (F + V - 1) / V;
-  const bool col = c < chunks;
+  const bool col = c * V < F;
   const int64_t step = (int64_t)gridDim.x * GROUPS;
   // groups of one CTA take the same number of trips: those past the last row stay for the shuffles
   for (int64_t row0 = (int64_t)blockIdx.x * GROUPS; row0 < rows; row0 += step * R) {
@@ -42,8 +41,7 @@ __global__ void __launch_bounds__(256) quantize_rows_kernel(const T *__restrict_
       for (int j = 0; j < V; ++j) m = max(m, abs_bits(f[j]));
       const Scale s = block_scale(lanes_max<LANES>(m));
       if (row < rows) {
-        if (col) store_e4m3(Y8 + row * ld8 + (int64_t)c * V, f, s.inv);
-        if (c == chunks - 1) zero_to_boundary<V>(Y8 + row * ld8, chunks);
+        if (col) store_e4m3<V>(Y8 + row * ld8, c, F, f, s.inv);
         if (lane == 0) scales[(int64_t)b * lds + row] = s.s;
       }
     }
@@ -85,7 +83,7 @@ __global__ void __launch_bounds__(256) quantize_weight_kernel(const T *__restric
 #pragma unroll
   for (int i = 0; i < 16; ++i) {
     const int r = r0 + y + 8 * i;
-    const uint32_t q = pack_e4m3x4_scaled(f[i], s.inv);
+    const uint32_t q = keep_bytes(pack_e4m3x4_scaled(f[i], s.inv), r < R ? C - c0 - 4 * x : 0);   // zeros outside, also by a scale of NaN
     tile[y + 8 * i][x] = q;
     // a group of four bytes is inside or outside as a whole
     if (W8 && r < R && c0 + 4 * x < end) *reinterpret_cast<uint32_t *>(W8 + (int64_t)r * ld8 + c0 + 4 * x) = q;
