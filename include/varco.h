@@ -279,9 +279,9 @@ int varco_workspace_status(const void *workspace, void *stream, int *device_stat
  * nodes, in any order.
  *
  * 8-bit form.  A matrix in 8 bits is a matrix of e4m3 bytes (`ld` in elements = bytes, a multiple of 16, base 16-byte
- * aligned) and 32-bit scales: value = byte value * scale.  A block's scale is s = max|x| / 448 (not below 2^-126) and
- * its bytes are round-to-nearest-even(x * (1/s)), saturated at +-448.  A block that holds a NaN or an infinity becomes
- * NaN (its finite values too, since one scale covers them).
+ * aligned) and 32-bit scales: value = byte value * scale.  A block's scale is s = max|x| * (1/448) (not below 2^-126) and
+ * its bytes are round-to-nearest-even(x * (1/s)), saturated at +-448, all in 32 bits with every operation rounded to nearest.
+ * A block that holds a NaN or an infinity becomes NaN through its scale (its finite values too, since one scale covers them).
  *   activations and gradients  one scale per row and 128 columns, stored [ceil(F/128) x lds]: the scale of row m and
  *                              column block b is scales[b * lds + m], lds >= rows
  *   weights                    one scale per 128 x 128 block

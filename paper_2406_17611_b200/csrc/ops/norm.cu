@@ -37,7 +37,8 @@ struct NormParams {
 // The 8-bit form of a team's row.  A 128-column block lies in neighbouring lanes of one chunk column, or, for teams
 // narrower than a block, in JB chunk columns of all lanes.
 template <typename T, int TEAM, int NCH, int V>
-__device__ __forceinline__ void quantize_row(const NormParams &p, int64_t row, int lane, int nchunks, const float (&f)[NCH][V]) {
+__device__ __forceinline__ void quantize_row(const NormParams &p, int64_t row, int lane, const float (&f)[NCH][V]) {
+  const int nchunks = chunks_of_eight<V>(p.F);
   constexpr int PER = kBlock / V, LANES = TEAM < PER ? TEAM : PER, JB = PER / LANES;
 #pragma unroll
   for (int j0 = 0; j0 < NCH; j0 += JB) {
@@ -52,7 +53,7 @@ __device__ __forceinline__ void quantize_row(const NormParams &p, int64_t row, i
     for (int j = j0; j < j0 + JB && j < NCH; ++j) {
       const int c = lane + j * TEAM;
       if (row < p.rows && c < nchunks) {
-        store_e4m3<V>(p.y8 + row * p.ld8, c, p.F, f[j], s.inv);
+        store_e4m3(p.y8 + row * p.ld8 + (int64_t)c * V, f[j], s.inv);
         if (c % PER == 0) p.scales[(int64_t)(c / PER) * p.lds + row] = s.s;
       }
     }
@@ -179,7 +180,7 @@ __global__ void __launch_bounds__(threads_per_cta<TEAM>()) norm_fwd_kernel(const
         clear_padding<V>(h[q][j], c, p.F);
         if (here && p.y) *reinterpret_cast<uint4 *>((T *)p.y + row * p.ldy + (int64_t)c * V) = pack16(h[q][j], T());
       }
-      if (p.y8) quantize_row<T, TEAM, NCH, V>(p, row, lane, nchunks, h[q]);
+      if (p.y8) quantize_row<T, TEAM, NCH, V>(p, row, lane, h[q]);
     }
   }
 }
@@ -254,7 +255,7 @@ __global__ void __launch_bounds__(threads_per_cta<TEAM>()) norm_bwd_kernel(const
       clear_padding<V>(t[j], c, p.F);
       if (here && p.y) *reinterpret_cast<uint4 *>((T *)p.y + row * p.ldy + (int64_t)c * V) = pack16(t[j], T());
     }
-    if (p.y8) quantize_row<T, TEAM, NCH, V>(p, row, lane, nchunks, t);
+    if (p.y8) quantize_row<T, TEAM, NCH, V>(p, row, lane, t);
     if (RES) rc.template load<T>(p.r, p.ldr, row + step, lane, TEAM, nchunks, more);
   }
   if (!p.dgain_part) return;
@@ -429,7 +430,7 @@ template <typename T> int forward(const NormParams &p, int sms, cudaStream_t st)
 #define F(TEAM, NCH) launch_fwd<T, TEAM, NCH>(p, sms, st)
   constexpr int V = ElemTraits<T>::kVec;
   const int nc = (p.F + V - 1) / V;
-  if (nc <= 2) return F(2, 1);
+  if (nc <= 2 && !(sizeof(T) == 4 && p.y8)) return F(2, 1);   // 16 bytes of an 8-bit row are four fp32 chunks: four lanes
   if (nc <= 4) return F(4, 1);
   if (p.r && nc <= 16) return launch_fwd_lanes<T, 8, 2>(p, nc, sms, st);
   if (p.r && nc <= 32) return launch_fwd_lanes<T, 16, 2>(p, nc, sms, st);

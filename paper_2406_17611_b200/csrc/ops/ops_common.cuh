@@ -12,7 +12,8 @@ constexpr float kLeastScale = 0x1p-126f;  // a block of zeros or denormals keeps
 
 // Scale of a block from the bits of its largest magnitude.  Magnitudes are compared as integers: for non-negative
 // floats the order is the same, and a NaN (bits above infinity's) wins, so that a block with a NaN is NaN as a
-// whole instead of losing it.
+// whole instead of losing it.  A scale that is not finite multiplies by zero: the block is NaN through its scale, its padding
+// stays zero.  1/s is rounded to nearest, so that the bytes are the definition's, ties included.
 struct Scale {
   float s, inv;
 };
@@ -20,7 +21,7 @@ __device__ __forceinline__ Scale block_scale(uint32_t amax_bits) {
   Scale r;
   r.s = __uint_as_float(amax_bits) * (1.f / kTop);
   if (r.s < kLeastScale) r.s = kLeastScale;
-  r.inv = __fdividef(1.f, r.s);       // s is at most 2^120: inside the range of the fast quotient, which rounds to 2 ulp
+  r.inv = __frcp_rn(fminf(r.s, __int_as_float(0x7F800000)));   // 0 where s is a NaN
   return r;
 }
 // max(v, 0) that keeps a NaN
@@ -54,26 +55,14 @@ __device__ __forceinline__ uint32_t pack_e4m3x4_scaled(float2 a, float2 b, float
 __device__ __forceinline__ uint32_t pack_e4m3x4_scaled(const float *f, float inv) {
   return pack_e4m3x4_scaled(make_float2(f[0], f[1]), make_float2(f[2], f[3]), inv);
 }
-// the first n bytes of a word, zeros behind them
-__device__ __forceinline__ uint32_t keep_bytes(uint32_t v, int n) { return n >= 4 ? v : n <= 0 ? 0u : v & ((1u << 8 * n) - 1u); }
-// Chunk c of a row of F columns in 8 bits, V columns a chunk.  What lies past F is zero, whatever the scale (a row's scale may be
-// NaN), and the last chunk takes the row to its next 16 bytes.
-template <int V> __device__ __forceinline__ void store_e4m3(uint8_t *row, int c, int F, const float (&f)[V], float inv) {
-  uint32_t w[V / 4];
-#pragma unroll
-  for (int i = 0; i < V / 4; ++i) w[i] = pack_e4m3x4_scaled(f + 4 * i, inv);
-  uint8_t *p = row + (int64_t)c * V;
-  const int left = F - c * V;
-  if (left < V) {
-#pragma unroll
-    for (int i = 0; i < V / 4; ++i) w[i] = keep_bytes(w[i], left - 4 * i);
-  }
-  if (V == 4) *reinterpret_cast<uint32_t *>(p) = w[0];
-  else *reinterpret_cast<uint2 *>(p) = make_uint2(w[0], w[V / 4 - 1]);
-  if (left <= V) {
-    for (int b = c * V + V; b % 16; b += 4) *reinterpret_cast<uint32_t *>(row + b) = 0u;
-  }
+__device__ __forceinline__ void store_e4m3(uint8_t *p, const float (&f)[4], float inv) {
+  *reinterpret_cast<uint32_t *>(p) = pack_e4m3x4_scaled(f, inv);
 }
+__device__ __forceinline__ void store_e4m3(uint8_t *p, const float (&f)[8], float inv) {
+  *reinterpret_cast<uint2 *>(p) = make_uint2(pack_e4m3x4_scaled(f, inv), pack_e4m3x4_scaled(f + 4, inv));
+}
+// Chunks of V bytes of an 8-bit row with its padding up to 16 bytes: those past the row's own hold zeros.
+template <int V> __device__ __forceinline__ int chunks_of_eight(int F) { return (F + 15) / 16 * (16 / V); }
 
 // A row is worked on by a team of TEAM threads: 2 to 32 lanes of a warp, or a whole CTA of TEAM threads.
 // Lane `l` holds the 16-byte chunks l, l + TEAM, ...: neighbouring lanes read neighbouring chunks.

@@ -20,6 +20,7 @@ __global__ void __launch_bounds__(256) quantize_rows_kernel(const T *__restrict_
   constexpr int V = ElemTraits<T>::kVec, LANES = kBlock / V, GROUPS = 256 / LANES, R = 4;   // R rows on their way
   const int lane = threadIdx.x % LANES, b = blockIdx.y, c = b * LANES + lane;
   const bool col = c * V < F;
+  const int chunks = chunks_of_eight<V>(F);
   const int64_t step = (int64_t)gridDim.x * GROUPS;
   // groups of one CTA take the same number of trips: those past the last row stay for the shuffles
   for (int64_t row0 = (int64_t)blockIdx.x * GROUPS; row0 < rows; row0 += step * R) {
@@ -30,20 +31,25 @@ __global__ void __launch_bounds__(256) quantize_rows_kernel(const T *__restrict_
       v[q] = make_uint4(0u, 0u, 0u, 0u);
       if (col && first + q * step < rows) v[q] = load_stream(reinterpret_cast<const uint4 *>(X + (first + q * step) * ldx) + c);
     }
+    float f[R][V];
+    uint32_t top = 0;
 #pragma unroll
     for (int q = 0; q < R; ++q) {
-      const int64_t row = first + q * step;
-      float f[V];
-      unpack16(v[q], f, T());
-      clear_padding<V>(f, c, F);
+      unpack16(v[q], f[q], T());
+      clear_padding<V>(f[q], c, F);
       uint32_t m = 0;
 #pragma unroll
-      for (int j = 0; j < V; ++j) m = max(m, abs_bits(f[j]));
-      const Scale s = block_scale(lanes_max<LANES>(m));
-      if (row < rows) {
-        if (col) store_e4m3<V>(Y8 + row * ld8, c, F, f, s.inv);
-        if (lane == 0) scales[(int64_t)b * lds + row] = s.s;
-      }
+      for (int j = 0; j < V; ++j) m = max(m, abs_bits(f[q][j]));
+      m = lanes_max<LANES>(m);
+      if (lane % R == q) top = m;
+    }
+    // lane q makes and stores row q's scale, so that its two quotients are taken once for the R rows
+    const Scale s = block_scale(top);
+    if (lane < R && first + lane * step < rows) scales[(int64_t)b * lds + first + lane * step] = s.s;
+#pragma unroll
+    for (int q = 0; q < R; ++q) {
+      const float inv = __shfl_sync(0xFFFFFFFFu, s.inv, q, LANES);
+      if (c < chunks && first + q * step < rows) store_e4m3(Y8 + (first + q * step) * ld8 + (int64_t)c * V, f[q], inv);
     }
   }
 }
@@ -83,7 +89,7 @@ __global__ void __launch_bounds__(256) quantize_weight_kernel(const T *__restric
 #pragma unroll
   for (int i = 0; i < 16; ++i) {
     const int r = r0 + y + 8 * i;
-    const uint32_t q = keep_bytes(pack_e4m3x4_scaled(f[i], s.inv), r < R ? C - c0 - 4 * x : 0);   // zeros outside, also by a scale of NaN
+    const uint32_t q = pack_e4m3x4_scaled(f[i], s.inv);
     tile[y + 8 * i][x] = q;
     // a group of four bytes is inside or outside as a whole
     if (W8 && r < R && c0 + 4 * x < end) *reinterpret_cast<uint32_t *>(W8 + (int64_t)r * ld8 + c0 + 4 * x) = q;

@@ -275,6 +275,46 @@ def test_quantize_weight(R, K, dtype):
     assert not out.data.view(torch.uint8)[:, K:].any() and not out.transposed.view(torch.uint8)[:, R:].any()
 
 
+def defined_eight(x, least=2.0 ** -126):
+    """(bytes, scales) of rows of 32-bit values by the definition, one IEEE operation after the other."""
+    rows, F = x.shape
+    nb = (F + 127) // 128
+    p = torch.nn.functional.pad(x, (0, nb * 128 - F)).view(rows, nb, 128)
+    s = (p.abs().amax(2) * torch.tensor(1 / 448, device=DEV)).clamp_min(least)
+    q = (p * (1 / s)[:, :, None]).clamp(-448.0, 448.0).to(E4M3).view(torch.uint8).view(rows, nb * 128)
+    return q[:, :F], s.t()
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16], ids=["f32", "bf16"])
+@pytest.mark.parametrize("rows,F", [(3000, 256), (777, 602), (60, 4100)])
+def test_eight_bits_are_the_definitions(rows, F, dtype):
+    """Bytes and scales bit for bit, over 60 binades and down to the least scale; ties (bf16 rows are full of them) to even."""
+    g = gen(rows)
+    x = randn(rows, F, g) * torch.exp2(torch.randint(-30, 30, (rows, 1), generator=g, device=DEV).float())
+    x[:9] *= 2.0 ** -100
+    X = matrix(x, dtype)
+    x = X[:, :F].float()
+    e = vb.varco_quantize_rows(X, F)
+    q, s = defined_eight(x)
+    assert torch.equal(e.scales, s) and torch.equal(e.data.view(torch.uint8)[:, :F], q)
+    w = vb.varco_quantize_weight(X[:, :F])
+    nr, nk = (rows + 127) // 128, (F + 127) // 128
+    p = torch.nn.functional.pad(x, (0, nk * 128 - F, 0, nr * 128 - rows)).view(nr, 128, nk, 128)
+    s = (p.abs().amax((1, 3)) * torch.tensor(1 / 448, device=DEV)).clamp_min(2.0 ** -126)
+    q = (p * (1 / s)[:, None, :, None]).clamp(-448.0, 448.0).to(E4M3).view(torch.uint8).view(nr * 128, nk * 128)[:rows, :F]
+    assert torch.equal(w.scales, s) and torch.equal(w.data.view(torch.uint8)[:, :F], q)
+    assert torch.equal(w.transposed.view(torch.uint8)[:, :rows], q.t())
+    if dtype == torch.float32:                            # the norm's and the product's outputs in 32 bits are what they quantise
+        n = vb.varco_norm_fwd(X, F, quantize=True)
+        q, s = defined_eight(n.Y[:, :F].contiguous())
+        assert torch.equal(n.scales, s) and torch.equal(n.Y8.view(torch.uint8)[:, :F], q)
+        B, _ = weight(F, F, g)
+        for M in (20, rows):
+            out = vb.varco_fp8_product(e.data[:M], e.scales[:, :M], B.data, B.scales, F, dtype=dtype, quantize=True, workspace=vb.varco_ops_workspace())
+            q, s = defined_eight(out.Y[:, :F].contiguous())
+            assert torch.equal(out.scales, s) and torch.equal(out.Y8.view(torch.uint8)[:, :F], q)
+
+
 # ------------------------------------------------------------------------------------------ product
 def operand(rows, F, g, extra=0, scale=1.0):
     """8-bit matrix with row-block scales whose padding bytes are NaN, its scales with a row stride of their own."""
