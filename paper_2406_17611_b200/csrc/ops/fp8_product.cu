@@ -329,17 +329,21 @@ __global__ void __launch_bounds__(CFG::kThreads, CFG::CTAS) fp8_product_kernel(c
       const int row0 = w.mt * kTileM + quarter * 32, nt = w.nt;
       const int col0 = nt * NT + part * COLS;
       const bool here = row0 < M && col0 < p.N;            // this warp has outputs in the tile
-      // The mask's pieces travel while the blocks are multiplied.
+      // The mask's pieces travel while the blocks are multiplied.  Columns past N are copied as zeros: their sums are scale x 0,
+      // NaN where the scale is not finite, and must not reach the block's magnitude (a row whose mask leaves nothing is zero
+      // whatever its operand holds; without a mask such a row's block is NaN all the same).
       auto load_mask = [&](int i0) {
 #pragma unroll
         for (int i = 0; i < PIECES; ++i) {
           const int j = lane % PARTS, c = col0 + (i0 + i) * SLAB + j * V;
-          if (i0 + i < NY && c < p.N) {
+          if (i0 + i < NY) {
+            const int bytes = min(V, max(p.N - c, 0)) * ES;
+            const T *from = (const T *)p.mask + (bytes ? c : 0);
 #pragma unroll
             for (int k = 0; k < PARTS; ++k) {
               const int r = k * (32 / PARTS) + lane / PARTS;
               const bool in = row0 + r < M;
-              copy16_async(stg + i * (32 * PARTS) + place<PARTS>(r, j), (const T *)p.mask + (int64_t)(in ? row0 + r : 0) * p.ldmask + c, in ? 16 : 0);
+              copy16_async(stg + i * (32 * PARTS) + place<PARTS>(r, j), from + (int64_t)(in ? row0 + r : 0) * p.ldmask, in ? bytes : 0);
             }
           }
         }
@@ -376,24 +380,22 @@ __global__ void __launch_bounds__(CFG::kThreads, CFG::CTAS) fp8_product_kernel(c
       if (p.mask && here) {
 #pragma unroll
         for (int i = 0; i < NY; ++i) {
-          if (col0 + i * SLAB < p.N) {
-            if (i % PIECES == 0) {
-              if (i > 0) {
-                __syncwarp();
-                load_mask(i);
-              }
-              copy_wait();
+          if (i % PIECES == 0) {
+            if (i > 0) {
               __syncwarp();
+              load_mask(i);
             }
+            copy_wait();
+            __syncwarp();
+          }
 #pragma unroll
-            for (int j = 0; j < PARTS; ++j) {
-              float f[V];
-              unpack16(stg[(i % PIECES) * (32 * PARTS) + place<PARTS>(lane, j)], f, T());
+          for (int j = 0; j < PARTS; ++j) {
+            float f[V];
+            unpack16(stg[(i % PIECES) * (32 * PARTS) + place<PARTS>(lane, j)], f, T());
 #pragma unroll
-              for (int k = 0; k < V; k += 2) {
-                float2 &a = acc[(i * SLAB + j * V + k) / 2];
-                a = make_float2(f[k] > 0.f ? a.x : 0.f, f[k + 1] > 0.f ? a.y : 0.f);
-              }
+            for (int k = 0; k < V; k += 2) {
+              float2 &a = acc[(i * SLAB + j * V + k) / 2];
+              a = make_float2(f[k] > 0.f ? a.x : 0.f, f[k + 1] > 0.f ? a.y : 0.f);
             }
           }
         }
@@ -401,13 +403,6 @@ __global__ void __launch_bounds__(CFG::kThreads, CFG::CTAS) fp8_product_kernel(c
       }
       float inv = 0.f;
       if (p.y8) {
-        if (col0 + COLS > p.N) {
-          // Columns past N are scale x 0: NaN where the scale is not finite, and the mask has no say there.  They must not
-          // reach the block's magnitude: a row whose mask leaves nothing is zero whatever its operand holds.
-#pragma unroll
-          for (int i = 0; i < COLS / 2; ++i)
-            acc[i] = make_float2(col0 + 2 * i < p.N ? acc[i].x : 0.f, col0 + 2 * i + 1 < p.N ? acc[i].y : 0.f);
-        }
         float t0 = 0.f, t1 = 0.f, t2 = 0.f, t3 = 0.f;
 #pragma unroll
         for (int i = 0; i < COLS / 2; i += 4) {
@@ -416,7 +411,7 @@ __global__ void __launch_bounds__(CFG::kThreads, CFG::CTAS) fp8_product_kernel(c
           t2 = max3<RELU>(acc[i + 2].x, acc[i + 2].y, t2);
           t3 = max3<RELU>(acc[i + 3].x, acc[i + 3].y, t3);
         }
-        uint32_t bits = abs_bits(max3<RELU>(t0, t1, max3<RELU>(t2, t3, 0.f)));
+        uint32_t bits = here ? abs_bits(max3<RELU>(t0, t1, max3<RELU>(t2, t3, 0.f))) : 0u;
         if (COLS < kBlock && NT >= kBlock) {   // the block's other half is in the warp four further: a named barrier for each pair
           uint32_t *e = exch + flip * (EPI * 32);
           flip ^= 1u;
