@@ -387,6 +387,33 @@ def test_fp8_product_few_rows(M, N, K):
     test_fp8_product(M, N, K, torch.bfloat16)
 
 
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32], ids=["bf16", "f32"])
+@pytest.mark.parametrize("M,N,K", [(20001, 100, 300), (40000, 128, 700), (19000, 65, 1300), (12001, 700, 1300), (5000, 513, 602), (9700, 256, 2100),
+                                   (19100, 1025, 140), (40001, 41, 602), (60000, 64, 1000), (38000, 1, 129), (1500, 900, 1100), (37, 3000, 520)])
+def test_fp8_product_many_tiles_and_blocks(M, N, K, dtype):
+    """Every tile form by value where a CTA works through several tiles of several blocks: accumulators in turn, operand stages
+    that wrap inside a tile, scales that change along K and from tile to tile, outputs that are ragged both ways.  Two CTAs of 128
+    columns (N of 65 to 128, more row tiles than SMs), one of 256, two of 64, one of 128."""
+    test_fp8_product(M, N, K, dtype)
+
+
+def test_fp8_product_values_repeat():
+    """Calls in a row give the same bits, and these are right."""
+    g = gen(26)
+    ws = vb.varco_ops_workspace()
+    for M, N, K in ((20001, 100, 700), (5000, 500, 700), (30000, 41, 300)):
+        A8, sA, a = operand(M, K, g)
+        B, b = weight(N, K, g)
+        outs = [vb.varco_fp8_product(A8, sA, B.data, B.scales, K, quantize=True, workspace=ws) for _ in range(5)]
+        y = a @ b.t()
+        e = product_error(a, b, K) + 2 * U * y.abs()
+        assert bool(((d64(outs[0].Y, N) - y).abs() <= e + 2.0 ** -8 * y.abs()).all())
+        check_eight(outs[0].Y8, outs[0].scales, y, e)
+        for o in outs[1:]:
+            assert torch.equal(o.Y[:, :N], outs[0].Y[:, :N]) and torch.equal(o.scales, outs[0].scales)
+            assert torch.equal(o.Y8.view(torch.uint8)[:, :N], outs[0].Y8.view(torch.uint8)[:, :N])
+
+
 def test_few_rows_clusters_that_start_apart():
     """The CTAs of a cluster exchange their rows' largest magnitudes.  Widths that leave a cluster's last CTAs without columns and
     more clusters than run at once, launched back to back: every call gives the first one's scales and bytes, and these are right."""
@@ -593,6 +620,50 @@ def test_a_single_row_that_ends_with_its_columns_is_refused_as_several_are():
     for n in (1, 2):
         with pytest.raises(vb.VarcoError):
             vb.varco_norm_fwd(torch.zeros((n, 60), dtype=torch.bfloat16, device=DEV), 60)
+
+
+# ------------------------------------------------------------------------------------------ graphs
+@pytest.mark.parametrize("rows", [5, 3000])
+def test_every_call_in_a_graph(rows):
+    """Calls captured in a CUDA graph, replayed on new inputs in the same buffers: what the calls themselves give for these."""
+    g = gen(rows)
+    width, hidden, dt = 300, 700, torch.bfloat16
+    ws, gws = vb.varco_ops_workspace(width), vb.varco_weight_grad_workspace(hidden, width)
+    X, R, G = matrix(randn(rows, width, g), dt), matrix(randn(rows, width, g), dt), torch.rand(width, generator=g, device=DEV) + 0.5
+    W = randn(hidden, width, g, 0.05)
+    P, C = W.clone(), W.bfloat16()
+
+    def step():
+        n = vb.varco_norm_fwd(X, width, gain=G, residual=R, quantize=True)
+        q = vb.varco_quantize_weight(W)
+        u = vb.varco_fp8_product(n.Y8, n.scales, q.data, q.scales, width, relu=True, quantize=True, workspace=ws)
+        d = vb.varco_fp8_product(u.Y8, u.scales, q.transposed, q.scales.t(), hidden, workspace=ws)
+        b = vb.varco_norm_bwd(d.Y, n.H, n.rstd, width, gain=G, residual_grad=R, quantize=True, workspace=ws)
+        dW, db = vb.varco_weight_grad(u.Y, hidden, n.Y, width, gws)
+        e = vb.varco_quantize_rows(b.dX, width)
+        norm = vb.varco_grad_norm([dW, db], ws)
+        vb.varco_clip_step([P], [dW], 0.1, 1.0, copies=[C], workspace=ws)
+        vb.varco_grad_clip([db], 0.5, ws)
+        return [n.Y8.view(torch.uint8)[:, :width], u.Y[:, :hidden], u.scales, b.dX[:, :width], b.dgain, dW, db, e.scales, norm, P, C]
+
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.stream(side):
+        step()
+        torch.cuda.synchronize()
+        with torch.cuda.graph(graph, stream=side):
+            out = step()
+    torch.cuda.synchronize()
+    for seed in (1, 2):
+        X[:, :width] = randn(rows, width, gen(seed)).to(dt)
+        P.copy_(W), C.copy_(W)
+        graph.replay()
+        got = [t.clone() for t in out]
+        P.copy_(W), C.copy_(W)
+        for a, b in zip(got, step()):
+            assert torch.equal(a, b)
+    assert vb.varco_workspace_status(ws) == 0 and vb.varco_workspace_status(gws) == 0
 
 
 # ------------------------------------------------------------------------------------------ refusals
