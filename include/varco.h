@@ -288,6 +288,7 @@ int varco_workspace_status(const void *workspace, void *stream, int *device_stat
  *
  * Padding.  An output's columns past the last one in use are written as zero up to the next 16 bytes, whatever its row holds;
  * columns behind them are left alone.  An input's padding may hold anything.
+ * Outputs overlap neither inputs nor one another, except where an operator works in place.
  *
  * Workspace.  Operators that take one want varco_ops_workspace_bytes bytes of device memory, zeroed once by the caller
  * before its first use and then passed to any number of calls, as long as these follow each other on one stream.
@@ -322,7 +323,8 @@ int varco_norm_bwd(const varco_norm_desc_t *desc, const void *dY, const void *H,
 /* varco_quantize_rows     the 8-bit form of X [rows x F] with row-block scales.
  * varco_quantize_weight   the 8-bit form of W [rows x cols] (ldw in elements, any alignment of the element) with 128 x 128
  *   scales [ceil(rows/128) x lds], lds >= ceil(cols/128): W8 [rows x ld8] and WT8 [cols x ldt8] (the transposed bytes;
- *   same scales with the two indexes exchanged).  Either may be NULL. */
+ *   same scales with the two indexes exchanged).  Either may be NULL.
+ *   Errors: INVALID_ARG, UNSUPPORTED (more than 8,388,480 columns of rows or rows of a weight; a weight's columns near 2^31), CUDA. */
 int varco_quantize_rows(int64_t rows, int32_t F, varco_dtype_t dtype, const void *X, int64_t ldx, void *Y8, int64_t ld8,
                         float *scales, int64_t lds, void *stream);
 int varco_quantize_weight(int32_t rows, int32_t cols, varco_dtype_t dtype, const void *W, int64_t ldw, void *W8, int64_t ld8,
@@ -334,7 +336,8 @@ int varco_quantize_weight(int32_t rows, int32_t cols, varco_dtype_t dtype, const
  *   layer input, where that is a ReLU's output.
  *   bias [N] fp32 or NULL; mask [M x N] of `dtype` or NULL (a NaN counts as not positive).  Outputs, one may be NULL: Y
  *   [M x N] of `dtype`; Y8 [M x N] + sY, its 8-bit form with row-block scales (of the unrounded values).
- *   Blocks are added by the tensor cores, scaled and summed over the blocks in 32-bit registers; no atomics.
+ *   Blocks are added by the tensor cores, scaled and summed over the blocks in 32-bit registers; no atomics.  The product of a
+ *   row's and a block's scale is taken first and has to be a 32-bit number itself.
  *   Errors: INVALID_ARG, WORKSPACE_TOO_SMALL, UNSUPPORTED (a size near 2^31), CUDA. */
 typedef struct {
   int64_t M;

@@ -120,12 +120,13 @@ int varco_quantize_rows(int64_t rows, int32_t F, varco_dtype_t dtype, const void
   if (rows < 0 || F < 1 || !dtype_ok(dtype)) return VARCO_INVALID_ARG;
   if (rows == 0) return VARCO_OK;
   if (!matrix_ok(X, ldx, F, elem_size(dtype)) || !matrix_ok(Y8, ld8, F, 1) || !scales || lds < rows) return VARCO_INVALID_ARG;
-  const int blocks = (F + kBlock - 1) / kBlock, sms = sm_count();
-  if (sms <= 0) return VARCO_CUDA;
+  const int64_t blocks = ((int64_t)F + kBlock - 1) / kBlock;
   if (blocks > 65535) return VARCO_UNSUPPORTED;
+  const int sms = sm_count();
+  if (sms <= 0) return VARCO_CUDA;
   const int groups = dtype == VARCO_F32 ? 8 : 16;
   const int64_t ctas = (rows + groups - 1) / groups, most = ((int64_t)sms * 8 + blocks - 1) / blocks;
-  const dim3 grid((unsigned)(ctas < most ? ctas : most), blocks);
+  const dim3 grid((unsigned)(ctas < most ? ctas : most), (unsigned)blocks);
   cudaStream_t st = (cudaStream_t)stream;
   if (dtype == VARCO_F32)
     quantize_rows_kernel<float><<<grid, 256, 0, st>>>((const float *)X, ldx, rows, F, (uint8_t *)Y8, ld8, scales, lds);
@@ -138,9 +139,10 @@ int varco_quantize_rows(int64_t rows, int32_t F, varco_dtype_t dtype, const void
 int varco_quantize_weight(int32_t rows, int32_t cols, varco_dtype_t dtype, const void *W, int64_t ldw, void *W8, int64_t ld8,
                           void *WT8, int64_t ldt8, float *scales, int64_t lds, void *stream) {
   if (rows < 1 || cols < 1 || !dtype_ok(dtype) || !W || ldw < cols || (!W8 && !WT8) || !scales) return VARCO_INVALID_ARG;
-  if ((W8 && !matrix_ok(W8, ld8, cols, 1)) || (WT8 && !matrix_ok(WT8, ldt8, rows, 1)) || lds < (cols + kBlock - 1) / kBlock) return VARCO_INVALID_ARG;
-  const dim3 grid((cols + kBlock - 1) / kBlock, (rows + kBlock - 1) / kBlock);
-  if (grid.y > 65535) return VARCO_UNSUPPORTED;
+  const int64_t across = ((int64_t)cols + kBlock - 1) / kBlock, down = ((int64_t)rows + kBlock - 1) / kBlock;
+  if ((W8 && !matrix_ok(W8, ld8, cols, 1)) || (WT8 && !matrix_ok(WT8, ldt8, rows, 1)) || lds < across) return VARCO_INVALID_ARG;
+  if (down > 65535 || cols > INT32_MAX - kBlock) return VARCO_UNSUPPORTED;
+  const dim3 grid((unsigned)across, (unsigned)down);
   cudaStream_t st = (cudaStream_t)stream;
   const int64_t end = round_up64(cols, 16), endt = round_up64(rows, 16);
   if (dtype == VARCO_F32)

@@ -113,6 +113,17 @@ def test_quantise_and_weight_gradient_arguments():
     assert L.varco_weight_grad(1 << 31, 8, 8, 1, A, 8, A, 8, A, 0, A, 1 << 40, 0) == UNSUPPORTED
 
 
+def test_quantisers_refuse_what_their_grids_cannot_hold():
+    """Widths whose count of blocks passes 65,535, up to the largest number, where rounding up to a block overflows 32 bits."""
+    L = vb.lib()
+    top, ld = (1 << 31) - 1, 1 << 31
+    for F in (65535 * 128 + 1, top - 127, top - 126, top):
+        assert L.varco_quantize_rows(4, F, 1, A, ld, A, ld, A, 4, 0) == UNSUPPORTED, F
+        assert L.varco_quantize_weight(F, 4, 0, A, 4, A, 16, 0, 0, A, 1, 0) == UNSUPPORTED, F
+    assert L.varco_quantize_weight(4, top, 0, A, top, A, ld, 0, 0, A, (1 << 24) - 1, 0) == INVALID       # too few scales a row
+    assert L.varco_quantize_weight(4, top, 0, A, top, A, ld, 0, 0, A, 1 << 24, 0) == UNSUPPORTED
+
+
 def test_clip_arguments():
     L = vb.lib()
     big = 1 << 22
