@@ -85,7 +85,8 @@ class ResidualTrainer(Trainer):
     """Trainer whose hidden layers are followed by feed-forward blocks and whose steps are clipped: the norm over the
     averaged gradients of all weights (graph layers and blocks) is kept below max_norm.  `hidden`: the blocks' inner width;
     `blocks`: their initial arrays, one dict of FeedForward.init's form for every hidden layer (drawn from `seed` if None).
-    bf16 layers read bf16 copies that the step itself writes."""
+    bf16 layers read bf16 copies, the blocks' products 8-bit forms; the step renews both, and refresh() has to follow every other
+    change of the weights (a checkpoint that is read into them)."""
 
     def __init__(self, plan, widths, weights, bf16, hidden, max_norm=1.0, blocks=None, seed=0, device="cuda:0"):
         super().__init__(plan, widths, weights, bf16, device)
@@ -102,6 +103,15 @@ class ResidualTrainer(Trainer):
         self.blocks = [FeedForward(w, hidden, b, self.dt, self.op_ws, device) for w, b in zip(inner, blocks)]
         # what the layers read: the weights themselves, or the bf16 copies of the matrices
         self.low = [[None if w is None else w.to(torch.bfloat16) if bf16 and w.dim() == 2 else None for w in layer] for layer in self.W]
+
+    def refresh(self):
+        """The bf16 copies of the layers' weights and the 8-bit forms of the blocks' are made from the weights again."""
+        for layer, low in zip(self.W, self.low):
+            for w, c in zip(layer, low):
+                if c is not None:
+                    c.copy_(w)
+        for b in self.blocks:
+            b.refresh()
 
     def _read(self, l):
         return [w if c is None else c for w, c in zip(self.W[l], self.low[l])]
