@@ -425,7 +425,10 @@ template <typename T, int TEAM, int NCH> int launch_bwd(const NormParams &p, con
 // chunks a lane fill the team better where the row is ragged (bf16 300 wide: 16 x 3 5450, 32 x 2 3899; 602: 16 x 5 5467, a CTA
 // of 96 4600) and keep more loads on their way where there is no residual (602: 16 x 5 5696, a CTA of 96 3980; 1024: 32 x 4
 // 6091, a CTA of 128 4897); where the row fits, one or two are better (256: 16 x 2 6137, 8 x 4 5947; 512: 32 x 2 6131, 16 x 4
-// 5804; 1024: a CTA of 128 6160, 32 x 4 5816).
+// 5804; 1024: a CTA of 128 6160, 32 x 4 5816).  The borders, with a residual:
+//   bf16 58 chunks: 16 x 4 5265, 32 x 2 5191;  60: 5385, 5408;  62: 5322, 5389.  fp32 58: 5577, 5231;  64: 5966, 5911
+//   bf16 104 chunks: 32 x 4 5435, a CTA of 128 5305;  112: 5491, 5835;  120: 5429, 5684;  past 128, a CTA of 192: 130: 32 x 5 5225,
+//   4926;  144: 5513, 5424.  fp32 104: 5677, 5424;  112: 5738, 5781;  119: 5455, 5782;  130: 5424, 5768;  160: 5757, 6133
 template <typename T> int forward(const NormParams &p, int sms, cudaStream_t st) {
 #define F(TEAM, NCH) launch_fwd<T, TEAM, NCH>(p, sms, st)
   constexpr int V = ElemTraits<T>::kVec;
@@ -434,8 +437,8 @@ template <typename T> int forward(const NormParams &p, int sms, cudaStream_t st)
   if (nc <= 4) return F(4, 1);
   if (p.r && nc <= 16) return launch_fwd_lanes<T, 8, 2>(p, nc, sms, st);
   if (p.r && nc <= 32) return launch_fwd_lanes<T, 16, 2>(p, nc, sms, st);
-  if (p.r && nc >= 58 && nc <= 64) return F(32, 2);
-  if (!p.r || nc < 120 || (sizeof(T) == 2 && nc > 128)) {
+  if (sizeof(T) == 2 && p.r && nc >= 60 && nc <= 64) return F(32, 2);
+  if (!p.r || nc < 112 || (sizeof(T) == 2 && nc > 128)) {
     if (nc <= 40) return launch_fwd_lanes<T, 8, 5>(p, nc, sms, st);
     if (nc <= 80) return launch_fwd_lanes<T, 16, 5>(p, nc, sms, st);
     if (nc <= 160) return launch_fwd_lanes<T, 32, 5>(p, nc, sms, st);
