@@ -515,7 +515,7 @@ extern "C" int varco_fp8_product(const varco_fp8_desc_t *d, const void *A8, cons
   cudaStream_t st = (cudaStream_t)stream;
   const int sms = sm_count();
   if (sms <= 0) return VARCO_CUDA;
-  if (few_rows_pay(d->M, d->N, d->K, sms)) return varco_launch_fp8_few_rows(d, A8, sA, B8, sB, bias, mask, Y, Y8, sY, st);
+  if (few_rows_pay(d->M, d->N, d->K, Y8 != nullptr, sms)) return varco_launch_fp8_few_rows(d, A8, sA, B8, sB, bias, mask, Y, Y8, sY, st);
   ProductParams p;
   memset(&p, 0, sizeof(p));
   p.M = d->M, p.N = d->N, p.kblocks = (d->K + kTileK - 1) / kTileK;

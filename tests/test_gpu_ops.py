@@ -419,7 +419,8 @@ def test_few_rows_clusters_that_start_apart():
     more clusters than run at once, launched back to back: every call gives the first one's scales and bytes, and these are right."""
     g = gen(25)
     ws = vb.varco_ops_workspace()
-    for M, N, K in ((1, 9400, 128), (8, 4096, 64), (20, 1040, 3000), (32, 130, 16), (5, 17, 1)):
+    for M, N, K in ((1, 9400, 128), (8, 9400, 1100), (8, 8288, 64), (8, 8289, 64), (8, 4096, 64), (20, 1040, 3000), (32, 4144, 64),
+                    (32, 4145, 64), (32, 130, 16), (5, 17, 1)):
         A8, sA, a = operand(M, K, g)
         B, b = weight(N, K, g)
         outs = [vb.varco_fp8_product(A8, sA, B.data, B.scales, K, keep=False, quantize=True, workspace=ws) for _ in range(40)]
