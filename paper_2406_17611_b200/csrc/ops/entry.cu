@@ -9,7 +9,8 @@ namespace {
 using namespace vops;
 
 // The layer's weight-gradient kernel takes at most 1024 x 256 outputs: larger ones go in pieces, each reading its columns of
-// A and B again (2.45M rows, 256 x 1024: 1.8 ms = 0.72 PFLOP/s).
+// A and B again (bf16, 2.45M rows, 256 x 1024: 1.78 ms = 0.72 PFLOP/s; 169,343 rows, 256 x 256: 105 us; fp32, without tensor
+// cores: 563 us = 39 TFLOP/s).
 constexpr int kMaxRows = 1024, kMaxCols = 256;
 
 size_t piece_bytes(int Fa, int Fb) {

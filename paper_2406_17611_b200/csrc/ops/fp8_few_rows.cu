@@ -1,9 +1,10 @@
 // The 8-bit product for at most 32 rows (a few nodes asked for at inference time): bound by reading B once.
 //
 // A 128-row tile would multiply empty rows, which costs nothing, but gives an SM a whole tile's contraction: 1 x 4096 x 4096
-// keeps 32 of 148 SMs busy for 16 us, 6.3 here (32 rows: 12.7; 1 x 1024 x 256 with both outputs 3.3 against 5.0, 32 x 1024 x
-// 1024 5.0 against 6.8).  A CTA owns 16 columns and its eight warps share the contraction, block by block; a warp's lanes read 16 bytes of B each (64 contiguous bytes of a row) straight into registers, as the first
-// operand of mma.sync m16n8k32: 16 columns of the product x 8 rows of A.  The order of k inside an instruction is free as
+// keeps 32 of 148 SMs busy for 15 us, 4.9 here (5.9 with an 8-bit output; 32 rows: 10.8 and 12.2; 1 x 8192 x 256 with both outputs
+// 3.4 against 4.9, 32 x 4096 x 1024 4.7 against 6.3).  A CTA owns 16 columns and its eight warps share the contraction, block by
+// block; a warp's lanes read 16 bytes of B each (64 contiguous bytes of a row) straight into registers, as the first operand of
+// mma.sync m16n8k32: 16 columns of the product x 8 rows of A.  The order of k inside an instruction is free as
 // long as both operands agree, so lane l of a row takes bytes 16 l .. 16 l + 15 of it and uses them for two instructions.
 // A block's sum is scaled and added in 32 bits, the warps' sums are added in their order.  The 8-bit output needs the
 // largest magnitude of 128 columns: eight CTAs of a cluster exchange theirs through distributed shared memory.

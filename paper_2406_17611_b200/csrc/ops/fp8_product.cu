@@ -15,11 +15,13 @@
 //   EPI          TMA loads of the operands (128-byte swizzle)
 //   EPI + 1      tcgen05.mma, one thread
 //   EPI + 2, 3   scales: half of the rows each, loaded four blocks ahead in registers, handed over with the accumulator
-// Bound: with short contractions by what is written (2.45M x 1024 x 256 with both outputs: 1.66 ms, 4.6 TB/s written, where a
-// fill of 5 GB reaches 3.9).  With long ones by bringing the operands in (48 KB a block of 256 columns at 61 bytes a clock of
-// an SM: 800 clocks; 32 KB and 720 clocks on 32 SMs), next by the round of an accumulator (instructions 512, commit and wake
-// 170, add 450, hand back 100: 615 a block with two), not by the 512 clocks of instructions; and by the power cap (16,384 x
-// 4096 x 4096: 0.30 ms = 1.83 PFLOP/s in a burst, 0.34 ms sustained).
+// Bound: the SM's own work, not memory: times follow the SM clock (2.45M x 1024 x 256 with both outputs: 1640 us at 1965 MHz, 1955
+// back to back under the power cap at 1575 to 1665 MHz, while the norm, which HBM bounds, keeps its time).  A tile of two blocks
+// takes 6200 clocks at either clock; its epilogue warps add, take the maximum, pack, stage and store one after the other.
+// Long contractions (16,384 x 4096 x 4096: 295 us = 1.86 PFLOP/s in a burst, 342 us sustained): 1250 to 1310 clocks a block.
+// Known parts, none of which is that long: instructions 512; the round of an accumulator 1230 (instructions, commit and wake 170,
+// add 450, hand back 100), 615 a block with two; operands 800 with 64 CTAs at work (48 KB at 61 bytes a clock of an SM; with all 148
+// not measured).
 // Every mbarrier wait is bounded: on expiry the status word is set, every role runs to its end without waiting (the
 // outputs are then invalid), loads and instructions in flight are waited for (bounded as well), TMEM is released and the
 // kernel returns.

@@ -10,8 +10,8 @@
 //
 // Bound: HBM.  Each row is read once and stays in registers between the statistics and the outputs: a team of 2 to 32
 // lanes holds a row of up to 160 chunks of 16 bytes, a whole CTA a longer one, and the next row's loads are on their way
-// meanwhile.  2.45M x 256 bf16 with residual and 8-bit output: forward 935 us, backward 958 us (6.1 and 5.9 TB/s of the
-// 6.5 that a copy reaches); 233,000 x 602 fp32: 193 us (5.8).
+// meanwhile.  2.45M x 256 bf16 with residual and 8-bit output: forward 935 us, backward 931 us (6.1 TB/s of the 6.5
+// that a copy reaches); 233,000 x 602 fp32: 193 us (5.8).
 #include "ops_common.cuh"
 
 namespace {
@@ -372,9 +372,10 @@ struct GainGrad {
   float *out, *part;         // dgain (or nullptr) and the workspace's lines
   unsigned *arrived;         // in the workspace's status block, zeroed with it
 };
-// Whether the backward's last CTA adds the gain gradient's lines itself: while that takes it two rounds of loads.  One launch
-// less is 2 us of host time and as much on the GPU; a round is 0.7 us (2000 x 64, one round: GPU 5.0 against 5.2 us, back-to-back
-// calls 8.2 against 6.2; 1000 x 100, two: 5.1 and 6.1, 8.2 and 7.2; 8000 x 64, four: 6.6 and 7.7, 8.2 and 8.6).
+// Whether the backward's last CTA adds the gain gradient's lines itself: while that takes it two rounds of loads.  It costs the GPU
+// up to 1 us and saves the host a launch, which is what a small call waits for.  Last CTA against a second kernel: 2000 x 64, one
+// round: calls 6.2 and 8.2 us (GPU 5.0 and 4.7); 1000 x 100, two: 7.2 and 8.2 (6.0 and 5.0); 8000 x 64, four: 9.2 and 9.2 (7.7 and
+// 5.8).
 bool last_adds(int64_t lines, int F, int threads) {
   const int cols = (F + 31) / 32 * 32, wide = cols < threads ? cols : threads, slices = threads / wide;
   return lines > 1 && (cols + wide - 1) / wide * ((lines + slices * kLines - 1) / (slices * kLines)) <= 2;
@@ -448,8 +449,10 @@ template <typename T> int forward(const NormParams &p, int sms, cudaStream_t st)
 }
 
 // The backward holds a row three times (row, gradient, gain gradient): lanes take few values.  bf16 with a residual: one chunk
-// (256 wide: 32 x 1 5927, 16 x 2 4000; 512: a CTA of 64 5934, 32 x 2 3495); without one, and fp32, two (bf16 256: 16 x 2 5759, 32 x 1 5097; fp32 128: 16 x 2 6271, 32 x 1 6026).
-// CTAs of bf16 rows up to 4096 wide are faster with one chunk a thread than with two (2048: 348 against 463 us).
+// (256 wide: 32 x 1 5927, 16 x 2 4000; 512: a CTA of 64 5934, 32 x 2 3495); without one, and fp32, two (bf16 256: 16 x 2 5759,
+// 32 x 1 5097; fp32 128: 16 x 2 6271, 32 x 1 6026).  CTAs of bf16 rows up to 4096 wide are faster with one chunk a thread than with
+// two (2048: 348 against 463 us).  CTAs of 1024 threads have 64 registers a thread: rows past 8192
+// columns spill (16,384 wide: bf16 4.2, fp32 3.5 TB/s).
 template <typename T> int backward(const NormParams &p, const GainGrad &d, int sms, cudaStream_t st) {
 #define F(TEAM, NCH) launch_bwd<T, TEAM, NCH>(p, d, sms, st)
   constexpr int V = ElemTraits<T>::kVec;

@@ -1,11 +1,12 @@
 // 8-bit operands of the product: e4m3 values and 32-bit scales.
 //
-//   rows     one scale for every row and 128 columns (activations, gradients):  s = max|x| / 448, q = e4m3(x / s)
+//   rows     one scale for every row and 128 columns (activations, gradients):  s = max|x| (1/448), q = e4m3(x (1/s))
 //   weight   one scale for every 128 x 128 block, and both layouts of the bytes: the product contracts over the last
 //            index of both operands, so the forward reads W and the backward W transposed, each with the same scales
 //
 // Bound: HBM (rows: one pass, the next row's loads under the arithmetic; weight: a 128 x 128 block in registers, its
-// transposed bytes through shared memory).  2.45M x 256 bf16: 386 us (4.9 TB/s); 4096 x 4096 fp32, both layouts: 25 us (4.1 TB/s).
+// transposed bytes through shared memory).  2.45M x 256 bf16: 390 us (4.8 TB/s); 4096 x 4096, both layouts:
+// fp32 24 us (4.2 TB/s), bf16 27 (2.5: loads of single elements).
 #include "ops_common.cuh"
 
 namespace {
