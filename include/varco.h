@@ -301,7 +301,8 @@ int varco_ops_workspace_bytes(int32_t F_max, size_t *bytes);
 
 /* varco_norm_fwd    h = X + R (R may be NULL: h = X),  rstd = 1 / sqrt(mean(h^2) + eps),  y = gain . h . rstd
  *   X, R [rows x F] of `dtype`, gain [F] fp32 or NULL (ones).  Outputs, each may be NULL: H = h, Y = y (both `dtype`),
- *   Y8 + scales = y in 8 bits, rstd [rows] fp32.  All of it in 32 bits, from the unrounded sum, rounded once per output.
+ *   Y8 + scales = y in 8 bits, rstd [rows] fp32.  All of it in 32 bits, from the unrounded sum, rounded once per output
+ *   (the sum of a row's squares too: rows of values past 1.8e19 / sqrt(F) leave its range and come out as zero).
  * varco_norm_bwd    t = gain . dY,  dX = dRes + rstd (t - H rstd^2 mean(t . H)),  dgain = sum over rows of dY . H . rstd
  *   H, rstd from the forward; dRes NULL = 0.  dX is the gradient of both addends.  Outputs, each may be NULL: dX, dX8 +
  *   scales, dgain [F] fp32 (needs the workspace; summed in a fixed order).
@@ -368,8 +369,8 @@ int varco_weight_grad(int64_t rows, int32_t Fa, int32_t Fb, varco_dtype_t dtype,
  *                     0 elements are skipped); read during the call, not kept.  They must not overlap each other.  weights
  *                     and copies are host arrays of `num` addresses of as many elements; copies may be NULL.
  *   norm              device fp32, receives the norm (may be NULL except in varco_grad_norm).
- *   A norm of infinity gives c = 0 (an infinite gradient then makes its own weights NaN), a NaN makes everything NaN, as
- *   the formula says.  Squares are added so that the norm neither overflows nor underflows before it does itself; the
+ *   With a finite max_norm a norm of infinity gives c = 0 (an infinite gradient then makes its own weights NaN); a NaN makes
+ *   everything NaN, and so does an infinite norm with an infinite max_norm, as the formula says.  Squares are added so that the norm neither overflows nor underflows before it does itself; the
  *   order of the additions is fixed.  Up to 800 tensors take one cooperative launch.
  *   Errors: INVALID_ARG (eps <= 0, max_norm < 0, ...), WORKSPACE_TOO_SMALL, UNSUPPORTED (num > 16800), CUDA. */
 int varco_grad_norm(void *const *grads, const int64_t *counts, const int32_t *dtypes, int32_t num, float *norm, void *workspace,
